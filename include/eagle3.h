@@ -32,7 +32,8 @@ extern "C" {
 typedef struct eagle3_ctx eagle3_ctx;
 typedef void* eagle3_stream;              /* a hipStream_t; NULL = the default stream */
 
-enum { EAGLE3_FP32 = 0, EAGLE3_BF16 = 1 };
+enum { EAGLE3_FP32 = 0, EAGLE3_BF16 = 1,
+       EAGLE3_FP8 = 2 };                  /* e4m3 codes under a power-of-two scale; storage of paged caches only */
 
 enum {
   EAGLE3_OK = 0,
@@ -270,6 +271,99 @@ int eagle3_ttt_attention(int32_t dtype, int32_t T, int32_t n_heads, int32_t n_kv
 int eagle3_accept_static(int32_t B, int32_t N, int32_t vocab, const float* logits, const int32_t* tree_tok,
                          const int32_t* parent, float temperature, const float* uniforms,
                          int32_t* accept_len, int32_t* path, int32_t* bonus_tok, eagle3_stream stream);
+
+/* ---- rotary positions and a cache in pages ------------------------------------------------------
+ * For programs that run layers of their own around the calls above: plain decoding of single tokens, training steps, and
+ * sequences kept in pages of a pool, in 16, 32 or 8 bits.  None of these calls needs a context; like every call they enqueue
+ * kernels and return.  Arguments are checked; what lies in device memory (positions, lengths, page numbers) is not, and never
+ * leads outside the arrays described here. */
+
+/* Rotary angles.  Pair i < rot_dim / 2 of a head turns by positions * turns[i] full turns; the head's dimensions behind rot_dim stay
+ * as they are.  Angles are formed in 64 bits, so that far positions keep their fraction of a turn. */
+enum { EAGLE3_ROPE_PLAIN = 0, EAGLE3_ROPE_LINEAR = 1, EAGLE3_ROPE_PARTS = 2 };
+typedef struct {
+  const double* turns;      /* DEVICE [rot_dim / 2], as written by eagle3_rope_turns                      */
+  int32_t rot_dim;          /* even, 2 <= rot_dim <= head_dim                                             */
+  int32_t interleaved;      /* 0: pair i = dimensions (i, i + rot_dim / 2); 1: dimensions (2 i, 2 i + 1)  */
+  float amplitude;          /* factor on the rotated dimensions: 1 without a long-context correction      */
+} eagle3_rope_spec;
+
+/* HOST out [rot_dim / 2]: f_i = theta^(-2 i / rot_dim) / (2 pi) turns per position, scaled for contexts longer than those of training:
+ *   LINEAR  f_i / factor
+ *   PARTS   by how often a pair turns within original_len positions: f_i / factor up to `low` turns, f_i from `high` turns on, and
+ *           between them f_i (w + (1 - w) / factor) with w = (original_len f_i - low) / (high - low)
+ * Requires theta > 0, even rot_dim >= 2; LINEAR, PARTS: factor > 0; PARTS: original_len > 0 and low < high; all finite. */
+int eagle3_rope_turns(int32_t rot_dim, double theta, int32_t scaling, double factor, double low, double high, double original_len,
+                      double* out);
+
+/* Queries and keys of `rows` positions, rotated: (a, b) -> amplitude (a cos - b sin, b cos + a sin) for every pair, in 32 bits,
+ * rounded once.  With k NULL only q.
+ *   dtype       EAGLE3_BF16 or EAGLE3_FP32 of q and k
+ *   positions   DEVICE int32 [rows], any order
+ *   q, k        row r's heads [n_heads, head_dim] at q + r * q_stride elements (k likewise): q_stride >= n_heads * head_dim, so that
+ *               they may be parts of longer rows such as those of a joint q|k|v product
+ *   q_out       the same with a stride of its own; q_out == q with equal strides rotates in place, other overlaps are not allowed
+ * Requires rows, n_heads, n_kv_heads >= 1 and even head_dim <= 1024; rows * (n_heads + n_kv_heads) * head_dim < 2^40. */
+int eagle3_rope(int32_t dtype, int32_t rows, int32_t head_dim, const eagle3_rope_spec* rope, const int32_t* positions, int32_t n_heads,
+                const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int32_t n_kv_heads, const void* k, int64_t k_stride,
+                void* k_out, int64_t k_out_stride, eagle3_stream stream);
+
+/* The gradient of the above: from the gradients of the rotated q and k those of q and k (the same pairs turned back, times the
+ * amplitude).  Same arguments. */
+int eagle3_rope_grad(int32_t dtype, int32_t rows, int32_t head_dim, const eagle3_rope_spec* rope, const int32_t* positions, int32_t n_heads,
+                     const void* dq, int64_t dq_stride, void* dq_out, int64_t dq_out_stride, int32_t n_kv_heads, const void* dk,
+                     int64_t dk_stride, void* dk_out, int64_t dk_out_stride, eagle3_stream stream);
+
+/* One layer's cache in pages of a pool shared by B sequences: token p of sequence b lies in slot
+ * page_table[b][p / page_size] * page_size + p % page_size.  The arrays are those of a cache of n_pages * page_size slots as the
+ * calls above have it.  EAGLE3_FP8 holds bf16 rows in 8 bits: the row of a (slot, KV head) is head_dim codes and one exponent byte
+ * x, and a code c stands for the value e4m3(c) * 2^(x - 127), which bf16 holds exactly. */
+typedef struct {
+  void *k, *v;                            /* DEVICE [n_pages, page_size, n_kv_heads, head_dim], at multiples of 16 bytes       */
+  uint8_t *k_exp, *v_exp;                 /* DEVICE [n_pages, page_size, n_kv_heads]; EAGLE3_FP8 only, else NULL               */
+  const int32_t* page_table;              /* DEVICE [B, max_pages]; entries behind a sequence's last page are not read        */
+  int32_t dtype;                          /* EAGLE3_BF16, EAGLE3_FP32 or EAGLE3_FP8                                            */
+  int32_t n_pages, page_size, max_pages;  /* any sizes >= 1 with n_pages * page_size and max_pages * page_size < 2^31          */
+  int32_t n_kv_heads, head_dim;           /* head_dim 64 or 128                                                                */
+} eagle3_paged_kv;
+
+/* Writes new rows of B sequences behind what they hold: row j < n_new[b] of sequence b is its token start[b] + j.  Nothing but
+ * these slots is written; rows at negative positions, behind max_pages pages or on a page outside the pool are dropped.
+ * EAGLE3_FP8: per row the smallest power of two with which its largest finite magnitude is at most 448 (2^-110 at the least), codes
+ * rounded to nearest even (to 240 * 2^120 where 256 * 2^120 would be nearest, which is behind bf16's range); infinities and NaN are
+ * stored as NaN.
+ *   start, n_new   DEVICE int32 [B]; n_new NULL: `rows` of every sequence; n_new[b] is clamped to 0..rows
+ *   row_start      DEVICE int32 [B]: sequence b's row j is row row_start[b] + j of k_new and v_new, or NULL: row b * rows + j.  Rows
+ *                  outside 0..n_rows-1 are dropped
+ *   k_new, v_new   [n_rows] rows of [n_kv_heads, head_dim] bf16 (fp32 for an fp32 cache), row_stride elements apart; pointers and
+ *                  stride at multiples of 16 bytes
+ * Page tables may share pages; two rows of one call must not fall into the same slot. */
+int eagle3_paged_append(const eagle3_paged_kv* kv, int32_t B, int32_t rows, const int32_t* start, const int32_t* n_new,
+                        const int32_t* row_start, const void* k_new, const void* v_new, int64_t n_rows, int64_t row_stride,
+                        eagle3_stream stream);
+
+/* The way back: tokens start[b] .. start[b] + n[b] - 1 of every sequence as dense rows, bf16 (from EAGLE3_FP8 too, exactly) or fp32,
+ * for instance into an eagle3_kv's arrays, with its kv_indptr as row_start.  start NULL: from token 0; n NULL: `rows`; everything
+ * else as above.  Dropped rows and those that belong to no sequence keep what they hold. */
+int eagle3_paged_read(const eagle3_paged_kv* kv, int32_t B, int32_t rows, const int32_t* start, const int32_t* n, const int32_t* row_start,
+                      void* k_out, void* v_out, int64_t n_rows, int64_t row_stride, eagle3_stream stream);
+
+/* Attention of one new token of every sequence over its first kv_len[b] tokens (its own, appended before, among them):
+ * out = softmax(scale q K^T) V, and lse = the natural logarithm of the sum of exp(scale q K^T), with which parts of a context that were
+ * attended to separately are joined.
+ *   q          [B, n_heads, head_dim] bf16 (fp32 for an fp32 cache), sequence b's at q + b * q_stride elements; pointer and stride at
+ *              multiples of 16 bytes; query head h reads KV head h * n_kv_heads / n_heads
+ *   kv_len     DEVICE int32 [B], clamped to 0..max_kv_len; 0: out = 0, lse = -infinity
+ *   max_kv_len HOST bound >= 1, at most max_pages * page_size; sizes the launch
+ *   out        [B, n_heads, head_dim], dense, of q's type; lse fp32 [B, n_heads] or NULL
+ *   workspace  DEVICE, 256-byte aligned, of the bytes that the next call tells for the same sizes; NULL if these are 0.  Its content
+ *              need not be kept or cleared between calls; calls that may overlap in time need one each.
+ * Page numbers are clamped into the pool.  A sequence's infinite or NaN keys and values make its results NaN or infinite, no other's.
+ * Requires n_heads a multiple of n_kv_heads and B <= 65535. */
+int eagle3_paged_attention(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads, const void* q, int64_t q_stride, const int32_t* kv_len,
+                           int32_t max_kv_len, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                           eagle3_stream stream);
+int eagle3_paged_attention_workspace(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads, int32_t max_kv_len, size_t* bytes);
 
 #ifdef __cplusplus
 }

@@ -12,12 +12,14 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libeagle3.so")
-EAGLE3_FP32, EAGLE3_BF16 = 0, 1
+EAGLE3_FP32, EAGLE3_BF16, EAGLE3_FP8 = 0, 1, 2
 
 EXPORTS = ["eagle3_create", "eagle3_destroy", "eagle3_workspace_bytes", "eagle3_set_workspace", "eagle3_set_weights",
            "eagle3_strerror", "eagle3_last_error", "eagle3_profile_begin", "eagle3_profile_read", "eagle3_profile_end",
            "eagle3_fuse_features", "eagle3_draft_expand",
-           "eagle3_tree_verify", "eagle3_tree_verify_layers", "eagle3_accept", "eagle3_accept_static", "eagle3_commit", "eagle3_prefill", "eagle3_draft_chain", "eagle3_ttt_attention"]
+           "eagle3_tree_verify", "eagle3_tree_verify_layers", "eagle3_accept", "eagle3_accept_static", "eagle3_commit", "eagle3_prefill", "eagle3_draft_chain", "eagle3_ttt_attention",
+           "eagle3_rope_turns", "eagle3_rope", "eagle3_rope_grad", "eagle3_paged_append", "eagle3_paged_read", "eagle3_paged_attention",
+           "eagle3_paged_attention_workspace"]
 
 
 class Config(C.Structure):
@@ -48,6 +50,15 @@ class KV(C.Structure):
 
 class DraftDebug(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("pool_tok", "pool_parent", "pool_score", "frontier", "chosen")]
+
+
+class RopeSpec(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("amplitude", C.c_float)]
+
+
+class PagedKV(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_exp", "v_exp", "page_table")] + \
+               [(n, C.c_int32) for n in ("dtype", "n_pages", "page_size", "max_pages", "n_kv_heads", "head_dim")]
 
 
 _lib = None
@@ -93,6 +104,15 @@ def lib():
         L.eagle3_draft_chain.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(KV),
                                          C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
         L.eagle3_ttt_attention.argtypes = [C.c_int32] * 6 + [C.c_void_p] * 5
+        L.eagle3_rope_turns.argtypes = [C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4 + [C.c_void_p]
+        L.eagle3_rope.argtypes = [C.c_int32] * 3 + [C.POINTER(RopeSpec), C.c_void_p] + \
+            [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64] * 2 + [C.c_void_p]
+        L.eagle3_rope_grad.argtypes = L.eagle3_rope.argtypes
+        L.eagle3_paged_append.argtypes = [C.POINTER(PagedKV), C.c_int32, C.c_int32] + [C.c_void_p] * 5 + [C.c_int64] * 2 + [C.c_void_p]
+        L.eagle3_paged_read.argtypes = L.eagle3_paged_append.argtypes
+        L.eagle3_paged_attention.argtypes = [C.POINTER(PagedKV), C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_float,
+                                             C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.eagle3_paged_attention_workspace.argtypes = [C.POINTER(PagedKV), C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
         _lib = L
     return _lib
 
@@ -370,3 +390,163 @@ def eagle3_ttt_attention(q, k_steps, v_steps):
     _check(lib().eagle3_ttt_attention(dt, T, H, Hkv, d, s, _ptr(q), _ptr(k_steps, q.dtype), _ptr(v_steps, q.dtype), _ptr(out),
                                       _stream()))
     return out
+
+
+# ---- rotary positions and a cache in pages: calls without a context
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _arg(t, dtype, shape, device, what):
+    """The address of a dense tensor of this type, shape (None: any size) and device."""
+    _need(t.dtype == dtype and t.device == device and t.dim() == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape)) and
+          t.is_contiguous(), f"{what}: a dense {dtype} tensor {shape} on {device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows_arg(t, dtype, shape, device, what):
+    """The address and row stride of [rows, heads, d] rows, each dense, any distance apart."""
+    _need(t.dtype == dtype and t.device == device and t.dim() == 3 and all(n is None or n == m for n, m in zip(shape, t.shape)),
+          f"{what}: {dtype} rows {shape} on {device} are wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    rows, heads, d = t.shape
+    s0, s1, s2 = t.stride()
+    row = heads * d
+    _need((s2 == 1 or d == 1) and (s1 == d or heads == 1) and (s0 >= row or rows == 1), f"{what}: each row's heads have to lie one behind the other")
+    return t.data_ptr(), max(s0, row)
+
+
+def _gpu(device):
+    _need(device.type == "cuda", f"tensors on a GPU are wanted, got one on {device}")
+
+
+def _on(device, call, *args):
+    """The call on the device's own current stream, whichever device is current."""
+    if device.index == torch.cuda.current_device():
+        _check(call(*args, torch.cuda.current_stream(device).cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, torch.cuda.current_stream(device).cuda_stream))
+
+
+class Rope:
+    """Rotary angles of a model: the table that eagle3_rope reads, and how pairs are formed.  scaling: "none", "linear" or "parts"
+    (include/eagle3.h: eagle3_rope_turns)."""
+
+    def __init__(self, rot_dim, theta, *, interleaved=False, scaling="none", factor=1.0, low=1.0, high=4.0, original_len=8192, amplitude=1.0,
+                 device="cuda:0"):
+        _need(scaling in ("none", "linear", "parts"), f"scaling: none, linear or parts, got {scaling!r}")
+        _need(rot_dim >= 2 and rot_dim % 2 == 0, f"rot_dim has to be even and at least 2, got {rot_dim}")
+        turns = torch.empty(rot_dim // 2, dtype=torch.float64)
+        _check(lib().eagle3_rope_turns(int(rot_dim), float(theta), ("none", "linear", "parts").index(scaling), float(factor), float(low), float(high),
+                                       float(original_len), turns.data_ptr()))
+        self.turns = turns.to(device)
+        _gpu(self.turns.device)
+        self.c = RopeSpec(self.turns.data_ptr(), int(rot_dim), int(bool(interleaved)), float(amplitude))
+
+
+def _rotate(call, rope, positions, q, k, out):
+    dev = q.device
+    _gpu(dev)
+    _need(rope.turns.device == dev, "the table of angles lies on another device")
+    dt = {torch.bfloat16: EAGLE3_BF16, torch.float32: EAGLE3_FP32}.get(q.dtype)
+    _need(dt is not None and q.dim() == 3, f"bf16 or fp32 rows [rows, heads, d] are wanted, got {q.dtype} {tuple(q.shape)}")
+    rows, H, d = q.shape
+    pos = _arg(positions, torch.int32, (rows,), dev, "positions")
+    args = []
+    outs = out if isinstance(out, (tuple, list)) else (out, None)
+    _need(len(outs) == 2, "out: one tensor, or one for q and one for k")
+    made = []
+    for x, y, what in ((q, outs[0], "q"), (k, outs[1], "k")):
+        if x is None:
+            _need(y is None, "out: a place for k without k")
+            args += [0, None, 0, None, 0]
+            continue
+        p, stride = _rows_arg(x, q.dtype, (rows, None, d), dev, what)
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        yp, y_stride = _rows_arg(y, q.dtype, x.shape, dev, "out of " + what)
+        args += [x.shape[1], p, stride, yp, y_stride]
+        made.append(y)
+    _on(dev, call, dt, rows, d, rope.c, pos, *args)
+    return tuple(made) if k is not None else made[0]
+
+
+def eagle3_rope(rope, positions, q, k=None, out=None):
+    """q [rows, H, d] and k [rows, Hkv, d] (bf16 or fp32, rows any distance apart) turned to their positions (int32 [rows]).  `out`: where
+    to, e.g. (q, k) themselves; returns the rotated q, or (q, k)."""
+    return _rotate(lib().eagle3_rope, rope, positions, q, k, out)
+
+
+def eagle3_rope_grad(rope, positions, dq, dk=None, out=None):
+    """The gradients of eagle3_rope's q and k from those of its results."""
+    return _rotate(lib().eagle3_rope_grad, rope, positions, dq, dk, out)
+
+
+class PagedKVCache:
+    """One layer's paged cache: k, v [n_pages, page_size, Hkv, d] (bf16, fp32 or float8_e4m3fn), page_table int32 [B, max_pages]; for
+    float8_e4m3fn also the scale exponents k_exp, v_exp uint8 [n_pages, page_size, Hkv]."""
+
+    def __init__(self, k, v, page_table, k_exp=None, v_exp=None):
+        dts = {torch.bfloat16: EAGLE3_BF16, torch.float32: EAGLE3_FP32, torch.float8_e4m3fn: EAGLE3_FP8}
+        dev = k.device
+        _gpu(dev)
+        _need(k.dtype in dts and k.dim() == 4, f"a pool [n_pages, page_size, Hkv, d] of bf16, fp32 or float8_e4m3fn is wanted, got {k.dtype} {tuple(k.shape)}")
+        fp8 = k.dtype == torch.float8_e4m3fn
+        _need((k_exp is not None) == fp8 and (v_exp is not None) == fp8, "scale exponents belong to an 8-bit pool, and to no other")
+        self.k, self.v, self.k_exp, self.v_exp, self.page_table = k, v, k_exp, v_exp, page_table
+        self.row_dtype, self.device = torch.bfloat16 if fp8 else k.dtype, dev
+        exps = [_arg(x, torch.uint8, k.shape[:3], dev, "scale exponents") if fp8 else None for x in (k_exp, v_exp)]
+        self.B, max_pages = page_table.shape
+        self.c = PagedKV(_arg(k, k.dtype, k.shape, dev, "k"), _arg(v, k.dtype, k.shape, dev, "v"), *exps,
+                         _arg(page_table, torch.int32, page_table.shape, dev, "page_table"), dts[k.dtype], k.shape[0], k.shape[1], max_pages,
+                         k.shape[2], k.shape[3])
+        self.heads, self.d = k.shape[2], k.shape[3]
+
+
+def _paged_rows(call, cache, k, v, start, n, rows, row_start):
+    dev, B = cache.device, cache.B
+    kp, stride = _rows_arg(k, cache.row_dtype, (None, cache.heads, cache.d), dev, "k rows")
+    vp, v_stride = _rows_arg(v, cache.row_dtype, k.shape, dev, "v rows")
+    _need(stride == v_stride, "k and v rows have to lie equally far apart")
+    n_rows = k.shape[0]
+    if rows is None:
+        _need(row_start is None and n_rows % B == 0, "rows: the most rows of a sequence")
+        rows = n_rows // B
+    _need(row_start is not None or n_rows == B * rows, f"{B} sequences of {rows} rows are {B * rows}, got {n_rows}")
+    ptrs = [None if t is None else _arg(t, torch.int32, (B,), dev, what) for t, what in ((start, "start"), (n, "n"), (row_start, "row_start"))]
+    _on(dev, call, cache.c, B, rows, *ptrs, kp, vp, n_rows, stride)
+
+
+def eagle3_paged_append(cache, k_new, v_new, start, n_new=None, rows=None, row_start=None):
+    """Writes k_new, v_new [n_rows, Hkv, d] behind the sequences' first start[b] tokens: n_new[b] rows each (None: `rows`, by default
+    n_rows / B), sequence b's from row row_start[b] (None: b * rows) on."""
+    _paged_rows(lib().eagle3_paged_append, cache, k_new, v_new, start, n_new, rows, row_start)
+
+
+def eagle3_paged_read(cache, start=None, n=None, rows=None, row_start=None, out=None):
+    """Tokens start[b] .. start[b] + n[b] - 1 (None: from 0; `rows` of them) as dense rows.  `out`: (k, v) [n_rows, Hkv, d], of which only the
+    rows read are written; by default zeros with `rows` rows of every sequence.  Returns (k, v)."""
+    if out is None:
+        _need(rows is not None and row_start is None, "without out, rows and no row_start")
+        out = tuple(torch.zeros(cache.B * rows, cache.heads, cache.d, dtype=cache.row_dtype, device=cache.device) for _ in range(2))
+    _paged_rows(lib().eagle3_paged_read, cache, out[0], out[1], start, n, rows, row_start)
+    return tuple(out)
+
+
+def eagle3_paged_attention(cache, q, kv_len, max_kv_len, scale=None, out=None, want_lse=False):
+    """q [B, H, d] over each sequence's first kv_len[b] <= max_kv_len tokens; scale: 1 / sqrt(d) by default.  Returns out [B, H, d], with
+    want_lse also the log of the softmax's sum, fp32 [B, H]."""
+    dev, B = cache.device, cache.B
+    qp, stride = _rows_arg(q, cache.row_dtype, (B, None, cache.d), dev, "q")
+    H = q.shape[1]
+    if out is None:
+        out = torch.empty(B, H, cache.d, dtype=cache.row_dtype, device=dev)
+    lse = torch.empty(B, H, dtype=torch.float32, device=dev) if want_lse else None
+    need = C.c_size_t()
+    _check(lib().eagle3_paged_attention_workspace(cache.c, B, H, int(max_kv_len), need))
+    ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+    _on(dev, lib().eagle3_paged_attention, cache.c, B, H, qp, stride, _arg(kv_len, torch.int32, (B,), dev, "kv_len"), int(max_kv_len),
+        float(cache.d ** -0.5 if scale is None else scale), _arg(out, cache.row_dtype, (B, H, cache.d), dev, "out"),
+        None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), need.value)
+    return (out, lse) if want_lse else out

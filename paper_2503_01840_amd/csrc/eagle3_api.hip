@@ -14,6 +14,8 @@
 #include "causal_rules.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
+#include "paged.hpp"
+#include "rotary_turns.hpp"
 #include "wide_tiles.hpp"
 
 namespace {
@@ -774,6 +776,113 @@ int eagle3_commit(eagle3_ctx* ctx, int32_t B, int32_t N, const int32_t* tree_tok
   CK(launch_commit(kv->k, kv->v, c.n_layers, kv->kv_indptr, prefix_len, tree_tok, path, accept_len, bonus_tok, taps, B, N,
                    c.hidden, (int)(c.n_kv_heads * c.head_dim * ctx->act_size), rows, taps_new, tok_new, n_new,
                    draft_prefix_len, draft_rows, (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+// ---------------------------------------------------------------- rotary positions and a cache in pages
+int eagle3_rope_turns(int32_t rot_dim, double theta, int32_t scaling, double factor, double low, double high, double original_len,
+                      double* out) {
+  if (!out) return EAGLE3_E_NULL;
+  return rope_turns(rot_dim, theta, scaling, factor, low, high, original_len, out) ? EAGLE3_OK : EAGLE3_E_SHAPE;
+}
+
+static int rope_rows(int32_t dtype, int32_t rows, int32_t d, const eagle3_rope_spec* rope, const int32_t* positions, const RopeTensor& q,
+                     const RopeTensor& k, float sign, eagle3_stream stream) {
+  if (!rope || !rope->turns || !positions || !q.x || !q.y || (k.x && !k.y)) return EAGLE3_E_NULL;
+  if (dtype != EAGLE3_BF16 && dtype != EAGLE3_FP32) return EAGLE3_E_SHAPE;
+  if (rows < 1 || d < 2 || d > 1024 || d % 2 || rope->rot_dim < 2 || rope->rot_dim > d || rope->rot_dim % 2) return EAGLE3_E_SHAPE;
+  const RopeTensor* tensors[2] = {&q, &k};
+  for (const RopeTensor* t : tensors) {
+    if (!t->x) continue;
+    if (t->heads < 1 || t->stride < (int64_t)t->heads * d || t->y_stride < (int64_t)t->heads * d) return EAGLE3_E_SHAPE;
+    if (t->x == t->y && t->stride != t->y_stride) return EAGLE3_E_SHAPE;
+  }
+  const int64_t heads = (int64_t)q.heads + (k.x ? k.heads : 0);
+  if (heads * d >= (int64_t)1 << 30 || rows * heads * d >= (int64_t)1 << 40) return EAGLE3_E_SHAPE;
+  const RopeAngles a = {rope->turns, positions, rope->rot_dim, rope->interleaved != 0, rope->amplitude, sign};
+  CK(launch_rope(dtype == EAGLE3_BF16, q, k.x ? k : RopeTensor{}, a, rows, d, (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+int eagle3_rope(int32_t dtype, int32_t rows, int32_t head_dim, const eagle3_rope_spec* rope, const int32_t* positions, int32_t n_heads,
+                const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int32_t n_kv_heads, const void* k, int64_t k_stride,
+                void* k_out, int64_t k_out_stride, eagle3_stream stream) {
+  return rope_rows(dtype, rows, head_dim, rope, positions, {q, q_out, q_stride, q_out_stride, n_heads},
+                   {k, k_out, k_stride, k_out_stride, n_kv_heads}, 1.f, stream);
+}
+
+int eagle3_rope_grad(int32_t dtype, int32_t rows, int32_t head_dim, const eagle3_rope_spec* rope, const int32_t* positions, int32_t n_heads,
+                     const void* dq, int64_t dq_stride, void* dq_out, int64_t dq_out_stride, int32_t n_kv_heads, const void* dk,
+                     int64_t dk_stride, void* dk_out, int64_t dk_out_stride, eagle3_stream stream) {
+  return rope_rows(dtype, rows, head_dim, rope, positions, {dq, dq_out, dq_stride, dq_out_stride, n_heads},
+                   {dk, dk_out, dk_stride, dk_out_stride, n_kv_heads}, -1.f, stream);
+}
+
+// The kernels' view of a caller's cache.
+static int paged_view(const eagle3_paged_kv* kv, PagedView& c) {
+  if (!kv || !kv->k || !kv->v || !kv->page_table) return EAGLE3_E_NULL;
+  if (kv->dtype != EAGLE3_BF16 && kv->dtype != EAGLE3_FP32 && kv->dtype != EAGLE3_FP8) return EAGLE3_E_SHAPE;
+  if (kv->dtype == EAGLE3_FP8 && (!kv->k_exp || !kv->v_exp)) return EAGLE3_E_NULL;
+  if (kv->n_pages < 1 || kv->page_size < 1 || kv->max_pages < 1 || kv->n_kv_heads < 1 || (kv->head_dim != 64 && kv->head_dim != 128))
+    return EAGLE3_E_SHAPE;
+  if ((int64_t)kv->n_pages * kv->page_size > INT32_MAX || (int64_t)kv->max_pages * kv->page_size > INT32_MAX || kv->n_kv_heads > 65535)
+    return EAGLE3_E_SHAPE;
+  if (((uintptr_t)kv->k | (uintptr_t)kv->v) & 15) return EAGLE3_E_SHAPE;
+  c = {(char*)kv->k, (char*)kv->v, kv->k_exp, kv->v_exp, kv->page_table, kv->n_pages, kv->max_pages, kv->n_kv_heads, kv->head_dim,
+       kv->max_pages * kv->page_size, divisor(kv->page_size)};
+  return EAGLE3_OK;
+}
+
+static int paged_rows(const eagle3_paged_kv* kv, bool read, int32_t B, int32_t rows, const int32_t* start, const int32_t* n,
+                      const int32_t* row_start, void* k, void* v, int64_t n_rows, int64_t row_stride, eagle3_stream stream) {
+  PagedView c;
+  TRY(paged_view(kv, c));
+  if (!k || !v || (!read && !start)) return EAGLE3_E_NULL;
+  const int64_t size = kv->dtype == EAGLE3_FP32 ? 4 : 2, row = (int64_t)c.Hkv * c.d;
+  if (B < 1 || rows < 1 || n_rows < 1 || n_rows > INT32_MAX || (int64_t)B * rows * c.Hkv > INT32_MAX / 2) return EAGLE3_E_SHAPE;
+  if (row_stride < row || row_stride > INT64_MAX / 4 / n_rows || row_stride * size % 16 || (((uintptr_t)k | (uintptr_t)v) & 15)) return EAGLE3_E_SHAPE;
+  CK(launch_paged_rows(c, kv->dtype, read, B, rows, start, n, row_start, k, v, n_rows, row_stride * size, (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+int eagle3_paged_append(const eagle3_paged_kv* kv, int32_t B, int32_t rows, const int32_t* start, const int32_t* n_new,
+                        const int32_t* row_start, const void* k_new, const void* v_new, int64_t n_rows, int64_t row_stride,
+                        eagle3_stream stream) {
+  return paged_rows(kv, false, B, rows, start, n_new, row_start, (void*)k_new, (void*)v_new, n_rows, row_stride, stream);
+}
+
+int eagle3_paged_read(const eagle3_paged_kv* kv, int32_t B, int32_t rows, const int32_t* start, const int32_t* n, const int32_t* row_start,
+                      void* k_out, void* v_out, int64_t n_rows, int64_t row_stride, eagle3_stream stream) {
+  return paged_rows(kv, true, B, rows, start, n, row_start, k_out, v_out, n_rows, row_stride, stream);
+}
+
+// What the sizes of an attention call have to be.
+static int paged_attention_sizes(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads, int32_t max_kv_len, PagedView& c) {
+  TRY(paged_view(kv, c));
+  if (B < 1 || B > 65535 || n_heads < 1 || n_heads > 65535 || n_heads % c.Hkv || max_kv_len < 1 || max_kv_len > c.tokens) return EAGLE3_E_SHAPE;
+  return EAGLE3_OK;
+}
+
+int eagle3_paged_attention_workspace(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads, int32_t max_kv_len, size_t* bytes) {
+  if (!bytes) return EAGLE3_E_NULL;
+  PagedView c;
+  TRY(paged_attention_sizes(kv, B, n_heads, max_kv_len, c));
+  *bytes = paged_attention_workspace(B, n_heads, c.Hkv, c.d, max_kv_len);
+  return EAGLE3_OK;
+}
+
+int eagle3_paged_attention(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads, const void* q, int64_t q_stride, const int32_t* kv_len,
+                           int32_t max_kv_len, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                           eagle3_stream stream) {
+  if (!q || !kv_len || !out) return EAGLE3_E_NULL;
+  PagedView c;
+  TRY(paged_attention_sizes(kv, B, n_heads, max_kv_len, c));
+  const int64_t size = kv->dtype == EAGLE3_FP32 ? 4 : 2;
+  if (q_stride < (int64_t)n_heads * c.d || q_stride > INT64_MAX / 4 / B || q_stride * size % 16 || (((uintptr_t)q | (uintptr_t)out) & 15))
+    return EAGLE3_E_SHAPE;
+  const size_t need = paged_attention_workspace(B, n_heads, c.Hkv, c.d, max_kv_len);
+  if (need > workspace_bytes || (need && (!workspace || ((uintptr_t)workspace & 255)))) return EAGLE3_E_STATE;
+  CK(launch_paged_attention(c, kv->dtype, B, n_heads, q, q_stride, kv_len, max_kv_len, scale, out, lse, workspace, (hipStream_t)stream));
   return EAGLE3_OK;
 }
 

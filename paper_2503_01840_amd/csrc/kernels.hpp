@@ -215,3 +215,28 @@ hipError_t launch_ttt_attention(bool bf16, const void* q, const void* k, const v
 // cache rows, the chunk's own included, are written.  q [n, H, d] bf16, out fragment-major bf16 [n, H * d].
 hipError_t launch_prefill_attention(const void* q, const void* kcache, const void* vcache, const SeqInfo* seq, int n, int H, int Hkv,
                                     int d, void* out, hipStream_t st);
+
+// ---------------------------------------------------------------- rotary positions (rotary.hip)
+struct RopeTensor {         // heads of x, rotated, to y; strides from row to row in elements
+  const void* x;
+  void* y;
+  long long stride, y_stride;
+  int heads;                // 0: no tensor
+};
+struct RopeAngles {
+  const double* turns;      // [rot / 2] turns per position
+  const int32_t* positions;
+  int rot, interleaved;
+  float amplitude, sign;    // sign: -1 turns back
+};
+hipError_t launch_rope(bool bf16, const RopeTensor& q, const RopeTensor& k, const RopeAngles& a, int rows, int d, hipStream_t st);
+
+// ---------------------------------------------------------------- a cache in pages (paged.hip, paged_attention.hip)
+enum { PAGED_FP32 = 0, PAGED_BF16 = 1, PAGED_FP8 = 2 };
+struct PagedView;
+// Rows of B sequences to (read: from) their slots; dense rows row_bytes apart.
+hipError_t launch_paged_rows(const PagedView& c, int dtype, bool read, int B, int rows, const int32_t* start, const int32_t* n,
+                             const int32_t* row_start, void* k, void* v, long long n_rows, long long row_bytes, hipStream_t st);
+size_t paged_attention_workspace(int B, int H, int Hkv, int d, int max_len);
+hipError_t launch_paged_attention(const PagedView& c, int dtype, int B, int H, const void* q, long long q_stride, const int32_t* kv_len, int max_len,
+                                  float scale, void* out, float* lse, void* workspace, hipStream_t st);
