@@ -354,7 +354,7 @@ int eagle3_paged_read(const eagle3_paged_kv* kv, int32_t B, int32_t rows, const 
  *   q          [B, n_heads, head_dim] bf16 (fp32 for an fp32 cache), sequence b's at q + b * q_stride elements; pointer and stride at
  *              multiples of 16 bytes; query head h reads KV head h * n_kv_heads / n_heads
  *   kv_len     DEVICE int32 [B], clamped to 0..max_kv_len; 0: out = 0, lse = -infinity
- *   max_kv_len HOST bound >= 1, at most max_pages * page_size; sizes the launch
+ *   max_kv_len HOST bound >= 1, at most max_pages * page_size and 2^30; sizes the launch
  *   out        [B, n_heads, head_dim], dense, of q's type; lse fp32 [B, n_heads] or NULL
  *   workspace  DEVICE, 256-byte aligned, of the bytes that the next call tells for the same sizes; NULL if these are 0.  Its content
  *              need not be kept or cleared between calls; calls that may overlap in time need one each.

@@ -393,40 +393,48 @@ def eagle3_ttt_attention(q, k_steps, v_steps):
 
 
 # ---- rotary positions and a cache in pages: calls without a context
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+# These are called once and more a layer and decoding step, with little for the GPU to do in each: what follows looks at every argument, but puts
+# messages together only for those that are refused (25 -> 9 us a call of eagle3_rope, of which 5 are the launch).
+def _refuse(what, wanted, t):
+    raise ValueError(f"{what}: {wanted} is wanted, got " + (f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}" if isinstance(t, torch.Tensor) else repr(t)))
 
 
-def _arg(t, dtype, shape, device, what):
-    """The address of a dense tensor of this type, shape (None: any size) and device."""
-    _need(t.dtype == dtype and t.device == device and t.dim() == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape)) and
-          t.is_contiguous(), f"{what}: a dense {dtype} tensor {shape} on {device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+def _arg(t, dtype, shape, gpu, what):
+    """The address of a dense tensor of this type and shape on GPU number `gpu`."""
+    if t.dtype is not dtype or t.get_device() != gpu or t.shape != shape or not t.is_contiguous():
+        _refuse(what, f"a dense {dtype} tensor {tuple(shape)} on cuda:{gpu}", t)
     return t.data_ptr()
 
 
-def _rows_arg(t, dtype, shape, device, what):
-    """The address and row stride of [rows, heads, d] rows, each dense, any distance apart."""
-    _need(t.dtype == dtype and t.device == device and t.dim() == 3 and all(n is None or n == m for n, m in zip(shape, t.shape)),
-          f"{what}: {dtype} rows {shape} on {device} are wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    rows, heads, d = t.shape
-    s0, s1, s2 = t.stride()
-    row = heads * d
-    _need((s2 == 1 or d == 1) and (s1 == d or heads == 1) and (s0 >= row or rows == 1), f"{what}: each row's heads have to lie one behind the other")
-    return t.data_ptr(), max(s0, row)
+def _rows_arg(t, dtype, rows, heads, d, gpu, what):
+    """The address and row stride of [rows, heads, d] rows, each dense, any distance apart; heads None: any number."""
+    ok = t.dtype is dtype and t.get_device() == gpu and t.dim() == 3
+    if ok:
+        n, h, m = t.shape
+        s0, s1, s2 = t.stride()
+        ok = (rows is None or n == rows) and (heads is None or h == heads) and m == d and s2 == 1 and (s1 == d or h == 1) and (s0 >= h * d or n <= 1)
+    if not ok:
+        _refuse(what, f"{dtype} rows [{rows}, {heads}, {d}], each with its heads one behind the other, on cuda:{gpu}", t)
+    return t.data_ptr(), s0 if s0 > h * d else h * d
 
 
-def _gpu(device):
-    _need(device.type == "cuda", f"tensors on a GPU are wanted, got one on {device}")
+def _gpu_of(t, what):
+    gpu = t.get_device()
+    if gpu < 0:
+        _refuse(what, "a tensor on a GPU", t)
+    return gpu
 
 
-def _on(device, call, *args):
-    """The call on the device's own current stream, whichever device is current."""
-    if device.index == torch.cuda.current_device():
-        _check(call(*args, torch.cuda.current_stream(device).cuda_stream))
+def _on(gpu, call, *args):
+    """The call on that GPU's own current stream, whichever GPU is current."""
+    stream = torch._C._cuda_getCurrentRawStream(gpu)
+    if gpu == torch.cuda.current_device():
+        code = call(*args, stream)
     else:
-        with torch.cuda.device(device):
-            _check(call(*args, torch.cuda.current_stream(device).cuda_stream))
+        with torch.cuda.device(gpu):
+            code = call(*args, stream)
+    if code:
+        raise Eagle3Error(code)
 
 
 class Rope:
@@ -435,41 +443,45 @@ class Rope:
 
     def __init__(self, rot_dim, theta, *, interleaved=False, scaling="none", factor=1.0, low=1.0, high=4.0, original_len=8192, amplitude=1.0,
                  device="cuda:0"):
-        _need(scaling in ("none", "linear", "parts"), f"scaling: none, linear or parts, got {scaling!r}")
-        _need(rot_dim >= 2 and rot_dim % 2 == 0, f"rot_dim has to be even and at least 2, got {rot_dim}")
+        if scaling not in ("none", "linear", "parts"):
+            _refuse("scaling", "none, linear or parts", scaling)
+        if rot_dim < 2 or rot_dim % 2:
+            _refuse("rot_dim", "an even number of at least 2", rot_dim)
         turns = torch.empty(rot_dim // 2, dtype=torch.float64)
         _check(lib().eagle3_rope_turns(int(rot_dim), float(theta), ("none", "linear", "parts").index(scaling), float(factor), float(low), float(high),
                                        float(original_len), turns.data_ptr()))
         self.turns = turns.to(device)
-        _gpu(self.turns.device)
+        self.gpu = _gpu_of(self.turns, "device")
         self.c = RopeSpec(self.turns.data_ptr(), int(rot_dim), int(bool(interleaved)), float(amplitude))
 
 
+_ROPE_TYPES = {torch.bfloat16: EAGLE3_BF16, torch.float32: EAGLE3_FP32}
+
+
 def _rotate(call, rope, positions, q, k, out):
-    dev = q.device
-    _gpu(dev)
-    _need(rope.turns.device == dev, "the table of angles lies on another device")
-    dt = {torch.bfloat16: EAGLE3_BF16, torch.float32: EAGLE3_FP32}.get(q.dtype)
-    _need(dt is not None and q.dim() == 3, f"bf16 or fp32 rows [rows, heads, d] are wanted, got {q.dtype} {tuple(q.shape)}")
+    gpu, dtype = _gpu_of(q, "q"), q.dtype
+    code = _ROPE_TYPES.get(dtype)
+    if code is None or q.dim() != 3 or rope.gpu != gpu:
+        _refuse("q", f"bf16 or fp32 [rows, heads, d] on cuda:{rope.gpu}", q)
     rows, H, d = q.shape
-    pos = _arg(positions, torch.int32, (rows,), dev, "positions")
-    args = []
-    outs = out if isinstance(out, (tuple, list)) else (out, None)
-    _need(len(outs) == 2, "out: one tensor, or one for q and one for k")
-    made = []
-    for x, y, what in ((q, outs[0], "q"), (k, outs[1], "k")):
-        if x is None:
-            _need(y is None, "out: a place for k without k")
-            args += [0, None, 0, None, 0]
-            continue
-        p, stride = _rows_arg(x, q.dtype, (rows, None, d), dev, what)
-        if y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        yp, y_stride = _rows_arg(y, q.dtype, x.shape, dev, "out of " + what)
-        args += [x.shape[1], p, stride, yp, y_stride]
-        made.append(y)
-    _on(dev, call, dt, rows, d, rope.c, pos, *args)
-    return tuple(made) if k is not None else made[0]
+    pos = _arg(positions, torch.int32, (rows,), gpu, "positions")
+    qp, q_stride = _rows_arg(q, dtype, rows, H, d, gpu, "q")
+    q_out, k_out = out if isinstance(out, (tuple, list)) else (out, None)
+    if q_out is None:
+        q_out = torch.empty((rows, H, d), dtype=dtype, device=q.device)
+    qo, qo_stride = _rows_arg(q_out, dtype, rows, H, d, gpu, "out of q")
+    if k is None:
+        if k_out is not None:
+            _refuse("out of k", "None without k", k_out)
+        _on(gpu, call, code, rows, d, rope.c, pos, H, qp, q_stride, qo, qo_stride, 0, None, 0, None, 0)
+        return q_out
+    kp, k_stride = _rows_arg(k, dtype, rows, None, d, gpu, "k")
+    Hkv = k.shape[1]
+    if k_out is None:
+        k_out = torch.empty((rows, Hkv, d), dtype=dtype, device=q.device)
+    ko, ko_stride = _rows_arg(k_out, dtype, rows, Hkv, d, gpu, "out of k")
+    _on(gpu, call, code, rows, d, rope.c, pos, H, qp, q_stride, qo, qo_stride, Hkv, kp, k_stride, ko, ko_stride)
+    return q_out, k_out
 
 
 def eagle3_rope(rope, positions, q, k=None, out=None):
@@ -483,39 +495,47 @@ def eagle3_rope_grad(rope, positions, dq, dk=None, out=None):
     return _rotate(lib().eagle3_rope_grad, rope, positions, dq, dk, out)
 
 
+_POOL_TYPES = {torch.bfloat16: EAGLE3_BF16, torch.float32: EAGLE3_FP32, torch.float8_e4m3fn: EAGLE3_FP8}
+
+
 class PagedKVCache:
     """One layer's paged cache: k, v [n_pages, page_size, Hkv, d] (bf16, fp32 or float8_e4m3fn), page_table int32 [B, max_pages]; for
     float8_e4m3fn also the scale exponents k_exp, v_exp uint8 [n_pages, page_size, Hkv]."""
 
     def __init__(self, k, v, page_table, k_exp=None, v_exp=None):
-        dts = {torch.bfloat16: EAGLE3_BF16, torch.float32: EAGLE3_FP32, torch.float8_e4m3fn: EAGLE3_FP8}
-        dev = k.device
-        _gpu(dev)
-        _need(k.dtype in dts and k.dim() == 4, f"a pool [n_pages, page_size, Hkv, d] of bf16, fp32 or float8_e4m3fn is wanted, got {k.dtype} {tuple(k.shape)}")
+        gpu = _gpu_of(k, "k")
+        if k.dtype not in _POOL_TYPES or k.dim() != 4:
+            _refuse("k", "a pool [n_pages, page_size, Hkv, d] of bf16, fp32 or float8_e4m3fn", k)
         fp8 = k.dtype == torch.float8_e4m3fn
-        _need((k_exp is not None) == fp8 and (v_exp is not None) == fp8, "scale exponents belong to an 8-bit pool, and to no other")
+        if (k_exp is not None) != fp8 or (v_exp is not None) != fp8:
+            _refuse("k_exp, v_exp", "scale exponents for an 8-bit pool, None for any other", k_exp)
+        if page_table.dim() != 2:
+            _refuse("page_table", "int32 [B, max_pages]", page_table)
         self.k, self.v, self.k_exp, self.v_exp, self.page_table = k, v, k_exp, v_exp, page_table
-        self.row_dtype, self.device = torch.bfloat16 if fp8 else k.dtype, dev
-        exps = [_arg(x, torch.uint8, k.shape[:3], dev, "scale exponents") if fp8 else None for x in (k_exp, v_exp)]
+        self.row_dtype, self.gpu = torch.bfloat16 if fp8 else k.dtype, gpu
+        n_pages, page_size, self.heads, self.d = k.shape
         self.B, max_pages = page_table.shape
-        self.c = PagedKV(_arg(k, k.dtype, k.shape, dev, "k"), _arg(v, k.dtype, k.shape, dev, "v"), *exps,
-                         _arg(page_table, torch.int32, page_table.shape, dev, "page_table"), dts[k.dtype], k.shape[0], k.shape[1], max_pages,
-                         k.shape[2], k.shape[3])
-        self.heads, self.d = k.shape[2], k.shape[3]
+        exps = [_arg(x, torch.uint8, k.shape[:3], gpu, "scale exponents") if fp8 else None for x in (k_exp, v_exp)]
+        self.c = PagedKV(_arg(k, k.dtype, k.shape, gpu, "k"), _arg(v, k.dtype, k.shape, gpu, "v"), *exps,
+                         _arg(page_table, torch.int32, page_table.shape, gpu, "page_table"), _POOL_TYPES[k.dtype], n_pages, page_size, max_pages,
+                         self.heads, self.d)
 
 
 def _paged_rows(call, cache, k, v, start, n, rows, row_start):
-    dev, B = cache.device, cache.B
-    kp, stride = _rows_arg(k, cache.row_dtype, (None, cache.heads, cache.d), dev, "k rows")
-    vp, v_stride = _rows_arg(v, cache.row_dtype, k.shape, dev, "v rows")
-    _need(stride == v_stride, "k and v rows have to lie equally far apart")
+    gpu, B, i32 = cache.gpu, cache.B, torch.int32
+    kp, stride = _rows_arg(k, cache.row_dtype, None, cache.heads, cache.d, gpu, "k rows")
     n_rows = k.shape[0]
+    vp, v_stride = _rows_arg(v, cache.row_dtype, n_rows, cache.heads, cache.d, gpu, "v rows")
+    if stride != v_stride:
+        _refuse("v rows", "the row stride of the k rows", v)
     if rows is None:
-        _need(row_start is None and n_rows % B == 0, "rows: the most rows of a sequence")
         rows = n_rows // B
-    _need(row_start is not None or n_rows == B * rows, f"{B} sequences of {rows} rows are {B * rows}, got {n_rows}")
-    ptrs = [None if t is None else _arg(t, torch.int32, (B,), dev, what) for t, what in ((start, "start"), (n, "n"), (row_start, "row_start"))]
-    _on(dev, call, cache.c, B, rows, *ptrs, kp, vp, n_rows, stride)
+        if row_start is not None:
+            _refuse("rows", "with row_start the most rows of a sequence", rows)
+    if row_start is None and n_rows != B * rows:
+        _refuse("k rows", f"{rows} rows for each of {B} sequences", k)
+    _on(gpu, call, cache.c, B, rows, None if start is None else _arg(start, i32, (B,), gpu, "start"), None if n is None else _arg(n, i32, (B,), gpu, "n"),
+        None if row_start is None else _arg(row_start, i32, (B,), gpu, "row_start"), kp, vp, n_rows, stride)
 
 
 def eagle3_paged_append(cache, k_new, v_new, start, n_new=None, rows=None, row_start=None):
@@ -528,8 +548,9 @@ def eagle3_paged_read(cache, start=None, n=None, rows=None, row_start=None, out=
     """Tokens start[b] .. start[b] + n[b] - 1 (None: from 0; `rows` of them) as dense rows.  `out`: (k, v) [n_rows, Hkv, d], of which only the
     rows read are written; by default zeros with `rows` rows of every sequence.  Returns (k, v)."""
     if out is None:
-        _need(rows is not None and row_start is None, "without out, rows and no row_start")
-        out = tuple(torch.zeros(cache.B * rows, cache.heads, cache.d, dtype=cache.row_dtype, device=cache.device) for _ in range(2))
+        if rows is None or row_start is not None:
+            _refuse("rows", "without out, rows and no row_start", rows)
+        out = tuple(torch.zeros(cache.B * rows, cache.heads, cache.d, dtype=cache.row_dtype, device=cache.k.device) for _ in range(2))
     _paged_rows(lib().eagle3_paged_read, cache, out[0], out[1], start, n, rows, row_start)
     return tuple(out)
 
@@ -537,16 +558,17 @@ def eagle3_paged_read(cache, start=None, n=None, rows=None, row_start=None, out=
 def eagle3_paged_attention(cache, q, kv_len, max_kv_len, scale=None, out=None, want_lse=False):
     """q [B, H, d] over each sequence's first kv_len[b] <= max_kv_len tokens; scale: 1 / sqrt(d) by default.  Returns out [B, H, d], with
     want_lse also the log of the softmax's sum, fp32 [B, H]."""
-    dev, B = cache.device, cache.B
-    qp, stride = _rows_arg(q, cache.row_dtype, (B, None, cache.d), dev, "q")
+    gpu, B, d, dtype, L = cache.gpu, cache.B, cache.d, cache.row_dtype, lib()
+    qp, stride = _rows_arg(q, dtype, B, None, d, gpu, "q")
     H = q.shape[1]
     if out is None:
-        out = torch.empty(B, H, cache.d, dtype=cache.row_dtype, device=dev)
-    lse = torch.empty(B, H, dtype=torch.float32, device=dev) if want_lse else None
+        out = torch.empty((B, H, d), dtype=dtype, device=q.device)
+    lse = torch.empty((B, H), dtype=torch.float32, device=q.device) if want_lse else None
     need = C.c_size_t()
-    _check(lib().eagle3_paged_attention_workspace(cache.c, B, H, int(max_kv_len), need))
-    ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
-    _on(dev, lib().eagle3_paged_attention, cache.c, B, H, qp, stride, _arg(kv_len, torch.int32, (B,), dev, "kv_len"), int(max_kv_len),
-        float(cache.d ** -0.5 if scale is None else scale), _arg(out, cache.row_dtype, (B, H, cache.d), dev, "out"),
-        None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), need.value)
+    _check(L.eagle3_paged_attention_workspace(cache.c, B, H, max_kv_len, need))
+    need = need.value
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _on(gpu, L.eagle3_paged_attention, cache.c, B, H, qp, stride, _arg(kv_len, torch.int32, (B,), gpu, "kv_len"), max_kv_len,
+        d ** -0.5 if scale is None else scale, _arg(out, dtype, (B, H, d), gpu, "out"), None if lse is None else lse.data_ptr(),
+        None if ws is None else ws.data_ptr(), need)
     return (out, lse) if want_lse else out

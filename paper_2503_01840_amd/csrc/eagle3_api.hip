@@ -859,7 +859,7 @@ int eagle3_paged_read(const eagle3_paged_kv* kv, int32_t B, int32_t rows, const 
 // What the sizes of an attention call have to be.
 static int paged_attention_sizes(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads, int32_t max_kv_len, PagedView& c) {
   TRY(paged_view(kv, c));
-  if (B < 1 || B > 65535 || n_heads < 1 || n_heads > 65535 || n_heads % c.Hkv || max_kv_len < 1 || max_kv_len > c.tokens) return EAGLE3_E_SHAPE;
+  if (B < 1 || B > 65535 || n_heads < 1 || n_heads > 65535 || n_heads % c.Hkv || max_kv_len < 1 || max_kv_len > c.tokens || max_kv_len > 1 << 30) return EAGLE3_E_SHAPE;
   return EAGLE3_OK;
 }
 
@@ -882,7 +882,7 @@ int eagle3_paged_attention(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads
     return EAGLE3_E_SHAPE;
   const size_t need = paged_attention_workspace(B, n_heads, c.Hkv, c.d, max_kv_len);
   if (need > workspace_bytes || (need && (!workspace || ((uintptr_t)workspace & 255)))) return EAGLE3_E_STATE;
-  CK(launch_paged_attention(c, kv->dtype, B, n_heads, q, q_stride, kv_len, max_kv_len, scale, out, lse, workspace, (hipStream_t)stream));
+  CK(launch_paged_attention(c, kv->dtype, B, n_heads, q, q_stride * size, kv_len, max_kv_len, scale, out, lse, workspace, (hipStream_t)stream));
   return EAGLE3_OK;
 }
 

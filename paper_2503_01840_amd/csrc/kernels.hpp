@@ -238,5 +238,5 @@ struct PagedView;
 hipError_t launch_paged_rows(const PagedView& c, int dtype, bool read, int B, int rows, const int32_t* start, const int32_t* n,
                              const int32_t* row_start, void* k, void* v, long long n_rows, long long row_bytes, hipStream_t st);
 size_t paged_attention_workspace(int B, int H, int Hkv, int d, int max_len);
-hipError_t launch_paged_attention(const PagedView& c, int dtype, int B, int H, const void* q, long long q_stride, const int32_t* kv_len, int max_len,
+hipError_t launch_paged_attention(const PagedView& c, int dtype, int B, int H, const void* q, long long q_bytes, const int32_t* kv_len, int max_len,
                                   float scale, void* out, float* lse, void* workspace, hipStream_t st);
