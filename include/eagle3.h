@@ -337,7 +337,8 @@ typedef struct {
  *                  outside 0..n_rows-1 are dropped
  *   k_new, v_new   [n_rows] rows of [n_kv_heads, head_dim] bf16 (fp32 for an fp32 cache), row_stride elements apart; pointers and
  *                  stride at multiples of 16 bytes
- * Page tables may share pages; two rows of one call must not fall into the same slot. */
+ * Page tables may share pages; two rows of one call must not fall into the same slot.  Requires B, rows, n_rows >= 1 and
+ * B * rows * n_kv_heads < 2^26 - 8. */
 int eagle3_paged_append(const eagle3_paged_kv* kv, int32_t B, int32_t rows, const int32_t* start, const int32_t* n_new,
                         const int32_t* row_start, const void* k_new, const void* v_new, int64_t n_rows, int64_t row_stride,
                         eagle3_stream stream);

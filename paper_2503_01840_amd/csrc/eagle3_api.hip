@@ -839,7 +839,7 @@ static int paged_rows(const eagle3_paged_kv* kv, bool read, int32_t B, int32_t r
   TRY(paged_view(kv, c));
   if (!k || !v || (!read && !start)) return EAGLE3_E_NULL;
   const int64_t size = kv->dtype == EAGLE3_FP32 ? 4 : 2, row = (int64_t)c.Hkv * c.d;
-  if (B < 1 || rows < 1 || n_rows < 1 || n_rows > INT32_MAX || (int64_t)B * rows * c.Hkv > INT32_MAX / 2) return EAGLE3_E_SHAPE;
+  if (B < 1 || rows < 1 || n_rows < 1 || n_rows > INT32_MAX || (int64_t)B * rows * c.Hkv * 32 > INT32_MAX - 256) return EAGLE3_E_SHAPE;
   if (row_stride < row || row_stride > INT64_MAX / 4 / n_rows || row_stride * size % 16 || (((uintptr_t)k | (uintptr_t)v) & 15)) return EAGLE3_E_SHAPE;
   CK(launch_paged_rows(c, kv->dtype, read, B, rows, start, n, row_start, k, v, n_rows, row_stride * size, (hipStream_t)stream));
   return EAGLE3_OK;

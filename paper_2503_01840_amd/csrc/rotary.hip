@@ -1,22 +1,42 @@
 // Rotary positions of queries and keys, and their gradient.
+//
+// A wavefront has one row (or a part of its heads): each lane forms the sine and cosine of one pair's angle and puts them into LDS; then the lanes take
+// 16-byte pieces of the heads, in the half layout two pieces that belong together, four of them in flight.  The angle is a fraction of
+// a turn, position times turns per position in 64 bits less its whole part, so that the 32-bit sine and cosine of it are as good at position
+// 131071 as at position 1.  Bound by bytes: every row is read and written once.
+#include <algorithm>
+
 #include "common.hpp"
 #include "kernels.hpp"
 
 namespace {
 
-// One workgroup per row: the row's sines and cosines first, then every pair of every head.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int MAX_PAIRS = 512;
+
+// cosine and signed sine of pair i at this position, times the amplitude
+__device__ __forceinline__ void angle(const RopeAngles& a, double pos, int i, float* cs, float* sn) {
+  const double f = a.turns[i];
+  float s, c;
+  sincospif(2.f * (float)fma(pos, f, -rint(pos * f)), &s, &c);
+  cs[i] = a.amplitude * c;
+  sn[i] = a.sign * a.amplitude * s;
+}
+
+// One pair, rotated: the same bits in every kernel.
+__device__ __forceinline__ void turn(float xa, float xb, float c, float s, float& ya, float& yb) {
+  ya = fmaf(xa, c, -(xb * s));
+  yb = fmaf(xb, c, xa * s);
+}
+
+// Any sizes and addresses: one workgroup per row, one pair or unrotated dimension per thread and round.
 template <typename T>
-__global__ __launch_bounds__(256) void rope_kernel(RopeTensor q, RopeTensor k, RopeAngles a, int d) {
-  __shared__ float cs[512], sn[512];
+__global__ __launch_bounds__(256) void rope_any_kernel(RopeTensor q, RopeTensor k, RopeAngles a, int d) {
+  __shared__ float cs[MAX_PAIRS], sn[MAX_PAIRS];
   const int r = blockIdx.x, half = a.rot >> 1;
   const double pos = (double)a.positions[r];
-  for (int i = threadIdx.x; i < half; i += 256) {
-    const double t = pos * a.turns[i];
-    float s, c;
-    sincospif(2.f * (float)(t - rint(t)), &s, &c);
-    cs[i] = a.amplitude * c;
-    sn[i] = a.sign * a.amplitude * s;
-  }
+  for (int i = threadIdx.x; i < half; i += 256) angle(a, pos, i, cs, sn);
   __syncthreads();
   const int per_head = half + d - a.rot;            // pairs, then dimensions that stay
   for (int u = threadIdx.x; u < (q.heads + k.heads) * per_head; u += 256) {
@@ -28,18 +48,124 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeTensor q, RopeTensor k, R
     if (i < half) {
       const int ia = a.interleaved ? 2 * i : i, ib = a.interleaved ? 2 * i + 1 : i + half;
       const float xa = load_f32(x, ia), xb = load_f32(x, ib);
-      store_from_f32(y, ia, xa * cs[i] - xb * sn[i]);
-      store_from_f32(y, ib, xb * cs[i] + xa * sn[i]);
+      float ya, yb;
+      turn(xa, xb, cs[i], sn[i], ya, yb);
+      store_from_f32(y, ia, ya);
+      store_from_f32(y, ib, yb);
     } else {
       y[i + half] = x[i + half];
     }
   }
 }
 
+template <typename T> struct Piece { static constexpr int N = 16 / sizeof(T); };
+template <typename T> __device__ __forceinline__ float at(const u32x4& w, int i) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+  else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+}
+template <typename T> __device__ __forceinline__ u32x4 piece_of(const float* f) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f[i]);
+    else w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+  }
+  return w;
+}
+
+// Everything in whole 16-byte pieces.  per_head: tasks of a head, the first `turning` of them to be rotated (two pieces each in the half layout);
+// tasks of a row go over `share` wavefronts (gridDim.y).
+template <typename T, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void rope_kernel(RopeTensor q, RopeTensor k, RopeAngles a, int rows, int d, Divisor per_head, int turning, int share) {
+  constexpr int N = Piece<T>::N, U = 4;
+  __shared__ __attribute__((aligned(16))) float cs[4][MAX_PAIRS], sn[4][MAX_PAIRS];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = blockIdx.x * 4 + wave, half = a.rot >> 1;
+  if (r >= rows) return;
+  const int tasks = (q.heads + k.heads) * per_head.d, first = blockIdx.y * share, last = min(tasks, first + share);
+  const T* qx = (const T*)q.x + (size_t)r * q.stride;
+  const T* kx = (const T*)k.x + (size_t)r * k.stride;
+  T* qy = (T*)q.y + (size_t)r * q.y_stride;
+  T* ky = (T*)k.y + (size_t)r * k.y_stride;
+  bool ready = false;
+  for (int u0 = first; u0 < last; u0 += 64 * U) {
+    u32x4 lo[U], hi[U];
+    int task[U];
+    T* to[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int u = u0 + 64 * j + lane;
+      task[j] = -1;
+      if (u < last) {
+        const int h = u / per_head, t = u % per_head;
+        const bool is_k = h >= q.heads;
+        const size_t off = (size_t)(is_k ? h - q.heads : h) * d + t * N + (!INTERLEAVED && t >= turning ? half : 0);
+        const T* x = (is_k ? kx : qx) + off;
+        to[j] = (is_k ? ky : qy) + off;
+        task[j] = t;
+        lo[j] = *(const u32x4*)x;
+        if (!INTERLEAVED && t < turning) hi[j] = *(const u32x4*)(x + half);
+      }
+    }
+    if (!ready) {
+      const double pos = (double)a.positions[r];
+      for (int i = lane; i < half; i += 64) angle(a, pos, i, cs[wave], sn[wave]);
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      ready = true;
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int t = task[j];
+      if (t < 0) continue;
+      if (t >= turning) {
+        *(u32x4*)to[j] = lo[j];
+      } else if constexpr (INTERLEAVED) {
+        float f[N];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+          turn(at<T>(lo[j], 2 * i), at<T>(lo[j], 2 * i + 1), cs[wave][t * (N / 2) + i], sn[wave][t * (N / 2) + i], f[2 * i], f[2 * i + 1]);
+        }
+        *(u32x4*)to[j] = piece_of<T>(f);
+      } else {
+        float fa[N], fb[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          turn(at<T>(lo[j], i), at<T>(hi[j], i), cs[wave][t * N + i], sn[wave][t * N + i], fa[i], fb[i]);
+        }
+        *(u32x4*)to[j] = piece_of<T>(fa);
+        *(u32x4*)(to[j] + half) = piece_of<T>(fb);
+      }
+    }
+  }
+}
+
+bool aligned(const RopeTensor& t, int n, int size) {
+  return !t.x || ((((uintptr_t)t.x | (uintptr_t)t.y) & 15) == 0 && t.stride * size % 16 == 0 && t.y_stride * size % 16 == 0);
+}
+
+template <typename T>
+hipError_t launch(const RopeTensor& q, const RopeTensor& k, const RopeAngles& a, int rows, int d, hipStream_t st) {
+  constexpr int N = Piece<T>::N;
+  const int unit = a.interleaved ? a.rot : a.rot / 2;               // what turning pieces have to fill
+  if (d % N || unit % N || !aligned(q, N, sizeof(T)) || !aligned(k, N, sizeof(T))) {
+    hipLaunchKernelGGL(rope_any_kernel<T>, dim3(rows), dim3(256), 0, st, q, k, a, d);
+    return hipGetLastError();
+  }
+  const int turning = unit / N;
+  const bool in_place = q.x == q.y && (!k.x || k.x == k.y);         // then the rest of a head stays as it is
+  const int per_head = turning + (in_place ? 0 : (d - a.rot) / N), tasks = (q.heads + k.heads) * per_head;
+  // few rows: a row over several wavefronts, each with the row's angles of its own
+  const int most = (tasks + 63) / 64, want = std::max(1, std::min(most, 2048 / rows));
+  const int share = (most + want - 1) / want * 64;
+  const dim3 grid((rows + 3) / 4, (tasks + share - 1) / share);
+  if (a.interleaved) hipLaunchKernelGGL((rope_kernel<T, true>), grid, dim3(256), 0, st, q, k, a, rows, d, divisor(per_head), turning, share);
+  else hipLaunchKernelGGL((rope_kernel<T, false>), grid, dim3(256), 0, st, q, k, a, rows, d, divisor(per_head), turning, share);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_rope(bool bf16, const RopeTensor& q, const RopeTensor& k, const RopeAngles& a, int rows, int d, hipStream_t st) {
-  if (bf16) hipLaunchKernelGGL(rope_kernel<bf16_t>, dim3(rows), dim3(256), 0, st, q, k, a, d);
-  else hipLaunchKernelGGL(rope_kernel<float>, dim3(rows), dim3(256), 0, st, q, k, a, d);
-  return hipGetLastError();
+  return bf16 ? launch<bf16_t>(q, k, a, rows, d, st) : launch<float>(q, k, a, rows, d, st);
 }
