@@ -317,7 +317,7 @@ int eagle3_rope_grad(int32_t dtype, int32_t rows, int32_t head_dim, const eagle3
 /* One layer's cache in pages of a pool shared by B sequences: token p of sequence b lies in slot
  * page_table[b][p / page_size] * page_size + p % page_size.  The arrays are those of a cache of n_pages * page_size slots as the
  * calls above have it.  EAGLE3_FP8 holds bf16 rows in 8 bits: the row of a (slot, KV head) is head_dim codes and one exponent byte
- * x, and a code c stands for the value e4m3(c) * 2^(x - 127), which bf16 holds exactly. */
+ * x, and a code c stands for the value e4m3(c) * 2^(x - 127), which bf16 holds exactly; x is 1..254. */
 typedef struct {
   void *k, *v;                            /* DEVICE [n_pages, page_size, n_kv_heads, head_dim], at multiples of 16 bytes       */
   uint8_t *k_exp, *v_exp;                 /* DEVICE [n_pages, page_size, n_kv_heads]; EAGLE3_FP8 only, else NULL               */

@@ -20,7 +20,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int WAVES = 4;
+constexpr int WAVES = PAGED_WAVES;
 constexpr float SLACK = 8.f;              // the running maximum moves when a score exceeds it by more than 2^8
 
 struct AttnArgs {
@@ -28,14 +28,14 @@ struct AttnArgs {
   const char* q;
   long long q_stride;                     // in bytes
   const int32_t* kv_len;
-  int max_len, H, G, chunk, parts;
-  Divisor by_units;                       // KV heads x row tiles
-  Divisor by_heads;
+  int max_len, H, G, B, units;            // units: KV heads x row tiles
+  int ranges;                             // a launch over ranges: into how many all sequences' tiles are divided
+  Divisor by_units, by_heads;
   float scale_log2;
   void* out;
   float* lse;
-  float* part_o;                          // [B, H, parts, D]
-  float* part_ml;                         // [B, H, parts, 2]
+  float* part_o;                          // [ranges + B, H, D]: of range r and sequence b at r + b
+  float* part_ml;                         // [ranges + B, H, 2]
 };
 
 template <int I, int N, typename F> __device__ __forceinline__ void static_for(F&& f) {
@@ -49,6 +49,19 @@ template <int I, int N, typename F> __device__ __forceinline__ void static_for(F
 template <int E> __device__ __forceinline__ uint32_t bcast16(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x150 + E, 0xF, 0xF, true); }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// An address that every lane has, kept in scalar registers: a load then adds a lane's 32 bits to it by itself.
+typedef const char __attribute__((address_space(1)))* GlobalBytes;
+__device__ __forceinline__ GlobalBytes uniform(const char* p) {
+  GlobalBytes g = (GlobalBytes)(uintptr_t)p;
+  asm("" : "+s"(g));
+  return g;
+}
+__device__ __forceinline__ uint32_t in_place(uint32_t offset) {      // keeps the widening to 64 bits, and so the scalar base, at the load
+  asm("" : "+v"(offset));
+  return offset;
+}
+template <typename T> __device__ __forceinline__ T load_at(GlobalBytes p) { return *(const T __attribute__((address_space(1)))*)p; }
 
 // Two codes of a dword (low or high half) as bf16: times 2^k, exact.
 template <bool HIGH> __device__ __forceinline__ uint32_t bf16_of_codes(uint32_t w, float scale) {
@@ -66,29 +79,40 @@ struct Tile {                             // one tile's keys and values, as load
   static constexpr int KL = D * SIZE / 64, E = 4 * BLOCKS, VD = D * SIZE / 64;      // loads of a key row, value rows, dwords of a value row
   u32x4 k[BLOCKS][KL];
   uint32_t v[E][VD];
-  uint32_t exps;                          // 8 bits: lane (g, m): of key (g, m % 8), its key row's (m < 8) or value row's
+  uint32_t exps;                          // 8 bits: see load_exps
 };
 
-template <int TYPE, int D>
-__global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(AttnArgs p) {
-#pragma clang fp contract(off)            // a score and the maximum that it may be have to be the same number, however large
+// One (KV head, row tile) of one sequence: queries in registers, the running maximum, sum and output of the tiles that this wavefront has taken.
+// BLOCKED: pages are whole blocks of 16 keys, so that a block's page is looked up once, by scalar loads, and rows lie at fixed distances.
+template <int TYPE, int D, bool BLOCKED>
+struct Walk {
   typedef Tile<TYPE, D> T;
   typedef typename CacheType<TYPE>::row Row;
-  constexpr bool FP8 = TYPE == PAGED_FP8, F32 = TYPE == PAGED_FP32;
-  constexpr int BLOCKS = T::BLOCKS, E = T::E, KEYS = 16 * BLOCKS, NF = D / 16;      // NF: products over the values
-  constexpr int LDS_ROW = D + 4;
-  __shared__ float so[WAVES][PAGED_ROWS][LDS_ROW], sml[WAVES][PAGED_ROWS][2];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-  const int b = blockIdx.y, part = (int)blockIdx.x / p.by_units, unit = (int)blockIdx.x % p.by_units, hk = unit % p.by_heads, rt = unit / p.by_heads;
-  const int n = min(max(p.kv_len[b], 0), p.max_len);
-  const int begin = part * p.chunk, end = min(n, begin + p.chunk);
-  if (begin >= n && part > 0) return;
-  const int head0 = hk * p.G + rt * PAGED_ROWS, rows = min(PAGED_ROWS, p.G - rt * PAGED_ROWS);
-  const int n_tiles = (end - begin + KEYS - 1) / KEYS;
+  static constexpr bool FP8 = TYPE == PAGED_FP8, F32 = TYPE == PAGED_FP32;
+  static constexpr int BLOCKS = T::BLOCKS, E = T::E, KEYS = 16 * BLOCKS, NF = D / 16;      // NF: products over the values
+  static constexpr int KB = D * T::SIZE, VB = KB / 16;                                       // bytes of a row, and of a lane's part of a value row
 
-  // queries, in the order of the keys' dimensions
-  u32x4 q[T::SIZE == 1 ? 2 * T::KL : T::KL];
-  {
+  const AttnArgs& p;
+  const int lane, m, g;
+  int b, n, hk, head0, rows;
+  u32x4 q[FP8 ? 2 * T::KL : T::KL];
+  floatx4 o[NF];
+  float mx, l;                            // of query m; l: over this lane's keys
+  const int32_t* table;
+  uint32_t row_bytes;
+
+  __device__ __forceinline__ Walk(const AttnArgs& args) : p(args), lane(threadIdx.x & 63), m(threadIdx.x & 15), g((threadIdx.x & 63) >> 4) {
+    row_bytes = (uint32_t)p.c.Hkv * KB;
+  }
+
+  __device__ __forceinline__ void begin(int seq, int unit) {
+    b = seq;
+    hk = unit % p.by_heads;
+    const int rt = unit / p.by_heads;
+    head0 = hk * p.G + rt * PAGED_ROWS;
+    rows = min(PAGED_ROWS, p.G - rt * PAGED_ROWS);
+    table = p.c.table + (size_t)b * p.c.max_pages;
+    // in the order of the keys' dimensions
     const char* qrow = p.q + (long long)b * p.q_stride + (size_t)(head0 + min(m, rows - 1)) * (D * sizeof(Row));
 #pragma unroll
     for (int j = 0; j < (int)(sizeof(q) / 16); ++j) {
@@ -96,52 +120,92 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(AttnArgs p) {
       q[j] = *(const u32x4*)(qrow + at * sizeof(Row));
       if (m >= rows) q[j] = u32x4{0, 0, 0, 0};
     }
+#pragma unroll
+    for (int i = 0; i < NF; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    mx = -FLT_MAX;
+    l = 0.f;
   }
 
-  const int32_t* table = p.c.table + (size_t)b * p.c.max_pages;
-  const uint32_t row_bytes = (uint32_t)p.c.Hkv * (D * T::SIZE);
-  const char* kbase = p.c.k + (size_t)hk * (D * T::SIZE) + 16 * g;
-  const char* vbase = p.c.v + (size_t)hk * (D * T::SIZE) + m * (D * T::SIZE / 16);
-  const uint8_t* xbase = FP8 ? (m < 8 ? p.c.k_exp : p.c.v_exp) + hk : nullptr;
-  const int my_e = m % E, my_key = 16 * (my_e >> 2) + 4 * g + (my_e & 3);           // the key of a tile whose page this lane looks up
-  const int from_lane = 4 * (16 * (m >> 2) + (m & 3));                              // the lane that has key m of block 0 (of block 1: 4 lanes on), in bytes
+  // ---- where a tile's rows lie.  BLOCKED: the slots of the first keys of its blocks (uniform); else the slot of one key in every lane.
+  struct Place { int slot[BLOCKED ? BLOCKS : 1]; };
+  struct Entry { int page[BLOCKED ? BLOCKS : 1]; };
+  // Keys behind a sequence's end are looked up like any other: in the table's bounds, on a page within the pool, and never counted.  So the first tile is
+  // asked for before the length is known.
+  __device__ __forceinline__ int clamped(int key) const { return min(key, p.c.tokens - 1); }
+  __device__ __forceinline__ int lane_key(int tile) const {         // the key that this lane looks up
+    const int e = m % E;
+    return clamped(tile * KEYS + 16 * (e >> 2) + 4 * g + (e & 3));
+  }
+  __device__ __forceinline__ Entry entry_of(int tile) const {
+    Entry x;
+    if constexpr (BLOCKED) {
+#pragma unroll
+      for (int i = 0; i < BLOCKS; ++i)
+        x.page[i] = ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)table)[clamped(tile * KEYS + 16 * i) / p.c.page];
+    } else {
+      x.page[0] = table[lane_key(tile) / p.c.page];
+    }
+    return x;
+  }
+  __device__ __forceinline__ Place place_of(int tile, const Entry& x) const {
+    Place s;
+    if constexpr (BLOCKED) {
+#pragma unroll
+      for (int i = 0; i < BLOCKS; ++i)
+        s.slot[i] = min(max(x.page[i], 0), p.c.n_pages - 1) * p.c.page.d + (clamped(tile * KEYS + 16 * i) & ~15) % p.c.page;
+    } else {
+      s.slot[0] = min(max(x.page[0], 0), p.c.n_pages - 1) * p.c.page.d + lane_key(tile) % p.c.page;
+    }
+    return s;
+  }
 
-  auto slot_of = [&](int tile) {          // of this lane's key; keys behind the end repeat the last one
-    const int key = min(begin + tile * KEYS + my_key, end - 1);
-    const int page = min(max(table[key / p.c.page], 0), p.c.n_pages - 1);
-    return page * p.c.page.d + key % p.c.page;
-  };
-  auto load = [&](T& t, int slot) {
-    if constexpr (FP8) t.exps = xbase[(size_t)(uint32_t)slot * (uint32_t)p.c.Hkv];
+  // ---- loads
+  __device__ __forceinline__ int from_lane(int block) const { return 4 * (16 * (m >> 2) + (m & 3) + 4 * block); }     // of the lane that has key m of a block, in bytes
+  __device__ __forceinline__ uint32_t load_exps(const Place& s) const {      // lane (g, m): of key (g, m % 8), its key row's (m < 8) or value row's
+    if constexpr (!FP8) return 0;
+    const uint8_t* x = (m < 8 ? p.c.k_exp : p.c.v_exp) + hk;
+    if constexpr (BLOCKED) {
+      const int s0 = s.slot[0], s1 = s.slot[BLOCKS - 1];
+      const uint32_t slot = (uint32_t)(m & 4 ? s1 : s0) + (uint32_t)(4 * g + (m & 3));
+      return x[(uint64_t)slot * (uint32_t)p.c.Hkv];
+    } else {
+      return x[(uint64_t)(uint32_t)s.slot[0] * (uint32_t)p.c.Hkv];
+    }
+  }
+  __device__ __forceinline__ void load_k(T& t, const Place& s) const {
+    const uint32_t at = BLOCKED ? in_place((uint32_t)m * row_bytes + 16 * g) : 0;
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i) {
-      const uint32_t s = (uint32_t)__builtin_amdgcn_ds_bpermute(from_lane + 16 * i, slot);
-      const char* row = kbase + (uint64_t)s * row_bytes;
+      GlobalBytes row;
+      if constexpr (BLOCKED) row = uniform(p.c.k + (uint64_t)(uint32_t)s.slot[i] * row_bytes + (size_t)hk * KB) + at;
+      else row = (GlobalBytes)(uintptr_t)(p.c.k + (size_t)hk * KB + 16 * g + (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(from_lane(i), s.slot[0]) * row_bytes);
 #pragma unroll
-      for (int j = 0; j < T::KL; ++j) t.k[i][j] = *(const u32x4*)(row + 64 * j);
+      for (int j = 0; j < T::KL; ++j) t.k[i][j] = load_at<u32x4>(row + 64 * j);
     }
+  }
+  __device__ __forceinline__ void load_v(T& t, const Place& s) const {
+    const uint32_t at = BLOCKED ? in_place(4 * (uint32_t)g * row_bytes + m * VB) : 0;
     static_for<0, E>([&](auto e) {
-      const char* row = vbase + (uint64_t)bcast16<e>((uint32_t)slot) * row_bytes;
-      if constexpr (T::VD == 1) t.v[e][0] = *(const uint32_t*)row;
-      else if constexpr (T::VD == 2) *(u32x2*)t.v[e] = *(const u32x2*)row;
+      GlobalBytes row;
+      if constexpr (BLOCKED)
+        row = uniform(p.c.v + (uint64_t)((uint32_t)s.slot[e / 4] + e % 4) * row_bytes + (size_t)hk * KB) + at;
+      else row = (GlobalBytes)(uintptr_t)(p.c.v + (size_t)hk * KB + m * VB + (uint64_t)bcast16<e>((uint32_t)s.slot[0]) * row_bytes);
+      if constexpr (T::VD == 1) t.v[e][0] = load_at<uint32_t>(row);
+      else if constexpr (T::VD == 2) *(u32x2*)t.v[e] = load_at<u32x2>(row);
       else
 #pragma unroll
-        for (int j = 0; j < T::VD; j += 4) *(u32x4*)(t.v[e] + j) = *(const u32x4*)(row + 4 * j);
+        for (int j = 0; j < T::VD; j += 4) *(u32x4*)(t.v[e] + j) = load_at<u32x4>(row + 4 * j);
     });
-  };
+  }
 
-  floatx4 o[NF];
-#pragma unroll
-  for (int i = 0; i < NF; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-  float mx = -FLT_MAX, l = 0.f;           // of query m; l: over this lane's keys
-
-  auto work = [&](T& t, int tile) {
-    // scores of keys (g, e), e = 4 block + i
-    float x[E];
+  // ---- products
+  template <typename F> __device__ __forceinline__ void work(T& t, int tile, F&& keys_are_used) {
+#pragma clang fp contract(off)            // a score and the maximum that it may be have to be the same number, however large
+    float x[E];                           // scores of keys (g, e), e = 4 block + i
     float kscale[BLOCKS];
     if constexpr (FP8)
 #pragma unroll
-      for (int i = 0; i < BLOCKS; ++i) kscale[i] = exp_scale((uint32_t)__builtin_amdgcn_ds_bpermute(from_lane + 16 * i, (int)t.exps));
+      for (int i = 0; i < BLOCKS; ++i) kscale[i] = exp_scale((uint32_t)__builtin_amdgcn_ds_bpermute(from_lane(i), (int)t.exps));
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i) {
       floatx4 s = {0.f, 0.f, 0.f, 0.f};
@@ -165,7 +229,10 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(AttnArgs p) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[4 * i + r] = s[r] * p.scale_log2;
     }
-    const int left = end - begin - tile * KEYS;             // keys of this tile; uniform
+    __builtin_amdgcn_sched_barrier(0);
+    keys_are_used();
+    __builtin_amdgcn_sched_barrier(0);
+    const int left = n - tile * KEYS;     // keys of this tile; uniform
     if (left < KEYS) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -174,6 +241,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(AttnArgs p) {
 #pragma unroll
         for (int j = 0; j < T::VD; ++j) t.v[e][j] = seen ? t.v[e][j] : 0u;          // a weight of zero does not silence an infinity
       }
+      if (16 * (m >> 2 & 1) + 4 * g + (m & 3) >= left) t.exps = 127;                // nor what lies in the place of an exponent
     }
     float top = x[0];
 #pragma unroll
@@ -198,7 +266,9 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(AttnArgs p) {
 #pragma unroll
         for (int i = 0; i < NF; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[e][i]), w[e], o[i], 0, 0, 0);
     } else {
-      if constexpr (FP8) static_for<0, E>([&](auto e) { w[e] *= exp_scale(bcast16<8 + e>(t.exps)); });
+      if constexpr (FP8) {
+        static_for<0, E>([&](auto e) { w[e] *= exp_scale(bcast16<8 + e>(t.exps)); });
+      }
       // a weight as a head of 8 bits and a tail of 8 more; the tail of a weight above zero is above zero, so that an infinity stays one
       u32x4 head, tail;
 #pragma unroll
@@ -240,123 +310,255 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attn_kernel(AttnArgs p) {
         }
       }
     }
-  };
-
-  if (wave < n_tiles) {
-    T ta, tb;
-    int slot = slot_of(wave), next = slot_of(wave + WAVES);
-    load(ta, slot);
-    for (int t = wave;;) {
-      if (t + WAVES < n_tiles) load(tb, next);
-      next = slot_of(t + 2 * WAVES);
-      __builtin_amdgcn_sched_barrier(0);
-      work(ta, t);
-      if ((t += WAVES) >= n_tiles) break;
-      if (t + WAVES < n_tiles) load(ta, next);
-      next = slot_of(t + 2 * WAVES);
-      __builtin_amdgcn_sched_barrier(0);
-      work(tb, t);
-      if ((t += WAVES) >= n_tiles) break;
-    }
   }
-  l = xlane_sum_step<5>(xlane_sum_step<4>(l));
 
-  // the wavefronts' results, joined
-  if (m < rows) {
-    if (g == 0) { sml[wave][m][0] = mx; sml[wave][m][1] = l; }
+  // Tiles first, first + STEP, ... below last, of a sequence of len keys.  A tile's keys are asked for as soon as those of the one before are multiplied,
+  // its values likewise, and its table entries one tile earlier; ask() begins.
+  T t;
+  Entry next;
+  template <int STEP> __device__ __forceinline__ void ask(int first) {
+    const Place s = place_of(first, entry_of(first));
+    next = entry_of(first + STEP);
+    t.exps = load_exps(s);
+    load_k(t, s);
+    load_v(t, s);
+  }
+  template <int STEP> __device__ __forceinline__ void tiles(int first, int last, int len) {
+    n = len;
+    if (first >= last) return;
+    int i = first;
+    for (; i + STEP < last; i += STEP) {
+      const Place s = place_of(i + STEP, next);
+      next = entry_of(i + 2 * STEP);
+      uint32_t exps;
+      work(t, i, [&] {
+        exps = load_exps(s);
+        load_k(t, s);
+      });
+      load_v(t, s);
+      t.exps = exps;
+    }
+    work(t, i, [] {});
+    l = xlane_sum_step<5>(xlane_sum_step<4>(l));
+  }
+
+  // dimension NF * (4 g + r) + i of query m
+  template <typename F> __device__ __forceinline__ void each4(F&& f) const {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int i = 0; i < NF; ++i) so[wave][m][NF * (4 * g + r) + i] = o[i][r];
+      for (int i = 0; i < NF; i += 4) f(NF * (4 * g + r) + i, floatx4{o[i][r], o[i + 1][r], o[i + 2][r], o[i + 3][r]});
+  }
+};
+
+template <bool F32> __device__ __forceinline__ void store_out(const AttnArgs& p, size_t at, const floatx4& v) {
+  if constexpr (F32) *(floatx4*)((float*)p.out + at) = v;
+  else store4_plain((bf16_t*)p.out, at, v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ float lse_of(float mx, float l) { return (mx + log2f(l)) * 0.69314718055994531f; }
+__device__ __forceinline__ int length_of(const AttnArgs& p, int b) { return min(max(p.kv_len[b], 0), p.max_len); }
+
+// The results of a workgroup's wavefronts, joined: f(row, first of four dimensions, their sums, maximum, sum of weights).
+template <typename W, int D, typename F>
+__device__ __forceinline__ void join_team(const W& w, int wave, int active, F&& f) {
+  __shared__ __attribute__((aligned(16))) float so[WAVES][PAGED_ROWS][D + 4], sml[WAVES][PAGED_ROWS][2];
+  if (w.m < w.rows && wave < active) {
+    if (w.g == 0) { sml[wave][w.m][0] = w.mx; sml[wave][w.m][1] = w.l; }
+    w.each4([&](int d, const floatx4& v) { *(floatx4*)&so[wave][w.m][d] = v; });
   }
   __syncthreads();
-  const bool whole = n <= p.chunk;
-  for (int u = threadIdx.x; u < rows * (D / 4); u += 64 * WAVES) {
-    const int row = u / (D / 4), d4 = u % (D / 4) * 4;
-    float M = sml[0][row][0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sml[w][row][0]);
-    float L = 0.f;
+  for (int u = threadIdx.x; u < w.rows * (D / 4); u += 64 * WAVES) {
+    const int row = u / (D / 4), d = u % (D / 4) * 4;
+    float M = -FLT_MAX, L = 0.f;
+    for (int i = 0; i < active; ++i) M = fmaxf(M, sml[i][row][0]);
     floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      if (w < n_tiles) {
-        const float a = exp2_fast(sml[w][row][0] - M);
-        L += a * sml[w][row][1];
-        sum += a * *(const floatx4*)&so[w][row][d4];
-      }
+    for (int i = 0; i < active; ++i) {
+      const float a = exp2_fast(sml[i][row][0] - M);
+      L += a * sml[i][row][1];
+      sum += a * *(const floatx4*)&so[i][row][d];
     }
-    const size_t bh = (size_t)b * p.H + head0 + row;
-    if (whole) {
-      if (n == 0) sum = floatx4{0.f, 0.f, 0.f, 0.f};
-      else sum /= L;
-      if constexpr (F32) *(floatx4*)((float*)p.out + bh * D + d4) = sum;
-      else store4_plain((bf16_t*)p.out, bh * D + d4, sum[0], sum[1], sum[2], sum[3]);
-      if (d4 == 0 && p.lse != nullptr) p.lse[bh] = n == 0 ? -__builtin_huge_valf() : (M + log2f(L)) * 0.69314718055994531f;
-    } else {
-      *(floatx4*)(p.part_o + (bh * p.parts + part) * D + d4) = sum;
-      if (d4 == 0) *(float2*)(p.part_ml + (bh * p.parts + part) * 2) = make_float2(M, L);
-    }
+    f(row, d, sum, M, L);
   }
 }
 
-// One workgroup per (sequence, query head): its parts, D / 4 lanes to each.
+template <int D>
+__device__ __forceinline__ void store_part(const AttnArgs& p, int range, int b, int h, int d, const floatx4& sum, float M, float L) {
+  const size_t part = (size_t)(range + b) * p.H + h;
+  *(floatx4*)(p.part_o + part * D + d) = sum;
+  if (d == 0) *(float2*)(p.part_ml + part * 2) = make_float2(M, L);
+}
 template <bool F32, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs p) {
-  constexpr int LANES = D / 4, PER = 256 / LANES;
-  __shared__ float so[PER][D], sml[PER][2];
-  const int h = blockIdx.x, b = blockIdx.y, n = min(max(p.kv_len[b], 0), p.max_len);
-  const int parts = (n + p.chunk - 1) / p.chunk;
-  if (parts <= 1) return;
+__device__ __forceinline__ void store_result(const AttnArgs& p, int b, int h, int d, const floatx4& sum, float M, float L) {
   const size_t bh = (size_t)b * p.H + h;
-  const int at = threadIdx.x / LANES, d4 = threadIdx.x % LANES * 4;
+  store_out<F32>(p, bh * D + d, sum / L);
+  if (d == 0 && p.lse != nullptr) p.lse[bh] = lse_of(M, L);
+}
+template <bool F32, int D>
+__device__ __forceinline__ void store_nothing(const AttnArgs& p, int b, int h, int d) {            // of a sequence without a token
+  const size_t bh = (size_t)b * p.H + h;
+  store_out<F32>(p, bh * D + d, floatx4{0.f, 0.f, 0.f, 0.f});
+  if (d == 0 && p.lse != nullptr) p.lse[bh] = -__builtin_huge_valf();
+}
+
+// Short contexts: a workgroup per sequence and unit; one launch.
+template <int TYPE, int D, bool BLOCKED>
+__global__ __launch_bounds__(64 * WAVES) void paged_whole_kernel(AttnArgs p) {
+  typedef Walk<TYPE, D, BLOCKED> W;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = blockIdx.y;
+  W w(p);
+  w.begin(b, blockIdx.x);
+  w.template ask<WAVES>(wave);
+  const int n = length_of(p, b), n_tiles = (n + W::KEYS - 1) / W::KEYS;
+  w.template tiles<WAVES>(wave, n_tiles, n);
+  join_team<W, D>(w, wave, min(n_tiles, WAVES), [&](int row, int d, const floatx4& sum, float M, float L) {
+    if (n > 0) store_result<W::F32, D>(p, b, w.head0 + row, d, sum, M, L);
+    else store_nothing<W::F32, D>(p, b, w.head0 + row, d);
+  });
+}
+
+// Tiles of the sequences b0 .. b0 + 63, up to and with this lane's.
+template <int KEYS> __device__ __forceinline__ int scan_tiles(const AttnArgs& p, int b0) {
+  const int lane = threadIdx.x & 63;
+  int v = b0 + lane < p.B ? (length_of(p, b0 + lane) + KEYS - 1) / KEYS : 0;
+  // within 16 lanes from 1, 2, 4, 8 lanes below, then the sums of the 16 and 32 lanes before
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+// Longer contexts: all sequences' tiles in equal ranges; the parts of sequences that do not lie within one range are joined by the next kernel.
+// TEAM: a workgroup has a range of one unit.  Else a wavefront has, and the wavefronts of a workgroup have the units of one range after the other, so that together
+// they read whole rows.
+template <int TYPE, int D, bool BLOCKED, bool TEAM>
+__global__ __launch_bounds__(64 * WAVES) void paged_ranges_kernel(AttnArgs p) {
+  typedef Walk<TYPE, D, BLOCKED> W;
+  constexpr int STEP = TEAM ? WAVES : 1;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = TEAM ? blockIdx.x : (int)blockIdx.x * WAVES + wave;
+  const int range = at / p.by_units, unit = at % p.by_units, offset = TEAM ? wave : 0;
+  if (range >= p.ranges) return;
+  int scanned = scan_tiles<W::KEYS>(p, 0), total = __builtin_amdgcn_readlane(scanned, 63), b0 = 0;
+  for (int c = 64; c < p.B; c += 64) total += __builtin_amdgcn_readlane(scan_tiles<W::KEYS>(p, c), 63);
+  const int per = paged_tiles_of_range(total, p.ranges);
+  int x = range * per;                    // next tile, counted over all sequences
+  const int last = min(total, x + per);
+  W w(p);
+  while (x < last) {
+    for (int end; x >= (end = __builtin_amdgcn_readlane(scanned, 63));) scanned = end + scan_tiles<W::KEYS>(p, b0 += 64);
+    const int i = __builtin_ctzll(__ballot(scanned > x));    // the first sequence of these 64 that ends behind x
+    const int b = b0 + i, n = length_of(p, b), n_tiles = (n + W::KEYS - 1) / W::KEYS, ends = __builtin_amdgcn_readlane(scanned, i), starts = ends - n_tiles;
+    const int stop = min(ends, last), first = x - starts + offset, behind = stop - starts;
+    const bool whole = x == starts && stop == ends;
+    w.begin(b, unit);
+    if (first < behind) {
+      w.template ask<STEP>(first);
+      w.template tiles<STEP>(first, behind, n);
+    }
+    if constexpr (TEAM) {
+      join_team<W, D>(w, wave, min(stop - x, WAVES), [&](int row, int d, const floatx4& sum, float M, float L) {
+        if (whole) store_result<W::F32, D>(p, b, w.head0 + row, d, sum, M, L);
+        else store_part<D>(p, range, b, w.head0 + row, d, sum, M, L);
+      });
+      if (stop < last) __syncthreads();
+    } else if (w.m < w.rows) {
+      const int h = w.head0 + w.m;
+      if (whole) w.each4([&](int d, const floatx4& v) { store_result<W::F32, D>(p, b, h, d, v, w.mx, w.l); });
+      else w.each4([&](int d, const floatx4& v) { store_part<D>(p, range, b, h, d, v, w.mx, w.l); });
+    }
+    x = stop;
+  }
+}
+
+// The parts of a (sequence, query head), D / 4 lanes to each, JW wavefronts to a head; and the sequences without a token.
+template <int KEYS, bool F32, int D, int JW>
+__global__ __launch_bounds__(512) void paged_join_kernel(AttnArgs p) {
+  constexpr int LANES = D / 4, PER = 64 * JW / LANES, HEADS = 8 / JW;
+  __shared__ __attribute__((aligned(16))) float so[HEADS][PER][D], sml[HEADS][PER][2];
+  const int mine = threadIdx.x / (64 * JW), h = blockIdx.x * HEADS + mine, b = blockIdx.y, n = length_of(p, b);
+  const int at = threadIdx.x % (64 * JW) / LANES, d = threadIdx.x % LANES * 4;
+  int total = 0, ends = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    const int scanned = scan_tiles<KEYS>(p, b0);
+    if (b >= b0 && b < b0 + 64) ends = total + __builtin_amdgcn_readlane(scanned, b - b0);
+    total += __builtin_amdgcn_readlane(scanned, 63);
+  }
+  if (n == 0) {
+    if (at == 0 && h < p.H) store_nothing<F32, D>(p, b, h, d);
+    return;
+  }
+  const int per = paged_tiles_of_range(total, p.ranges), starts = ends - (n + KEYS - 1) / KEYS, first = paged_first_range(starts, per), parts = paged_last_range(ends, per) - first + 1;
+  if (parts <= 1) return;
+  const size_t part0 = (size_t)(first + b) * p.H + min(h, p.H - 1);
   float M = -FLT_MAX, L = 0.f;
   floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int i = at; i < parts; i += PER) {
-    const float2 ml = *(const float2*)(p.part_ml + (bh * p.parts + i) * 2);
-    const floatx4 v = *(const floatx4*)(p.part_o + (bh * p.parts + i) * D + d4);
-    const float to = fmaxf(M, ml.x), a = exp2_fast(M - to), c = exp2_fast(ml.x - to);
-    M = to;
-    L = L * a + ml.y * c;
-    sum = sum * a + v * c;
+  for (int i0 = at; i0 < parts; i0 += 4 * PER) {              // four parts in flight
+    float2 ml[4];
+    floatx4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const size_t part = part0 + (size_t)min(i0 + j * PER, parts - 1) * p.H;
+      ml[j] = *(const float2*)(p.part_ml + part * 2);
+      v[j] = *(const floatx4*)(p.part_o + part * D + d);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i0 + j * PER < parts) {
+        const float to = fmaxf(M, ml[j].x), a = exp2_fast(M - to), c = exp2_fast(ml[j].x - to);
+        M = to;
+        L = L * a + ml[j].y * c;
+        sum = sum * a + v[j] * c;
+      }
+    }
   }
-  *(floatx4*)&so[at][d4] = sum;
-  if (d4 == 0) { sml[at][0] = M; sml[at][1] = L; }
+  *(floatx4*)&so[mine][at][d] = sum;
+  if (d == 0) { sml[mine][at][0] = M; sml[mine][at][1] = L; }
   __syncthreads();
-  if (at > 0) return;
+  if (at > 0 || h >= p.H) return;
   for (int i = 1; i < min(PER, parts); ++i) {
-    const float to = fmaxf(M, sml[i][0]), a = exp2_fast(M - to), c = exp2_fast(sml[i][0] - to);
+    const float to = fmaxf(M, sml[mine][i][0]), a = exp2_fast(M - to), c = exp2_fast(sml[mine][i][0] - to);
     M = to;
-    L = L * a + sml[i][1] * c;
-    sum = sum * a + *(const floatx4*)&so[i][d4] * c;
+    L = L * a + sml[mine][i][1] * c;
+    sum = sum * a + *(const floatx4*)&so[mine][i][d] * c;
   }
-  sum /= L;
-  if constexpr (F32) *(floatx4*)((float*)p.out + bh * D + d4) = sum;
-  else store4_plain((bf16_t*)p.out, bh * D + d4, sum[0], sum[1], sum[2], sum[3]);
-  if (d4 == 0 && p.lse != nullptr) p.lse[bh] = (M + log2f(L)) * 0.69314718055994531f;
+  store_result<F32, D>(p, b, h, d, sum, M, L);
 }
 
-template <int TYPE, int D>
-hipError_t launch(const AttnArgs& a, int B, int units, hipStream_t st) {
-  hipLaunchKernelGGL((paged_attn_kernel<TYPE, D>), dim3(units * a.parts, B), dim3(64 * WAVES), 0, st, a);
-  if (a.parts > 1) hipLaunchKernelGGL((paged_join_kernel<TYPE == PAGED_FP32, D>), dim3(a.H, B), dim3(256), 0, st, a);
+template <int TYPE, int D, bool BLOCKED>
+hipError_t launch(const AttnArgs& a, const PagedSplit& s, hipStream_t st) {
+  if (s.ranges == 0) {
+    hipLaunchKernelGGL((paged_whole_kernel<TYPE, D, BLOCKED>), dim3(a.units, a.B), dim3(64 * WAVES), 0, st, a);
+    return hipGetLastError();
+  }
+  const int n = s.ranges * a.units;
+  if (s.team) hipLaunchKernelGGL((paged_ranges_kernel<TYPE, D, BLOCKED, true>), dim3(n), dim3(64 * WAVES), 0, st, a);
+  else hipLaunchKernelGGL((paged_ranges_kernel<TYPE, D, BLOCKED, false>), dim3((n + WAVES - 1) / WAVES), dim3(64 * WAVES), 0, st, a);
+  constexpr int KEYS = 16 * CacheType<TYPE>::BLOCKS;
+  constexpr bool F32 = TYPE == PAGED_FP32;
+  if (s.ranges / a.B > 16) hipLaunchKernelGGL((paged_join_kernel<KEYS, F32, D, 8>), dim3(a.H, a.B), dim3(512), 0, st, a);
+  else hipLaunchKernelGGL((paged_join_kernel<KEYS, F32, D, 1>), dim3((a.H + 7) / 8, a.B), dim3(512), 0, st, a);
   return hipGetLastError();
+}
+template <int TYPE, int D>
+hipError_t launch(const AttnArgs& a, const PagedSplit& s, hipStream_t st) {
+  return a.c.page.d % 16 == 0 ? launch<TYPE, D, true>(a, s, st) : launch<TYPE, D, false>(a, s, st);
 }
 
 }  // namespace
 
 size_t paged_attention_workspace(int B, int H, int Hkv, int d, int max_len) {
-  return paged_partial_floats(B, H, d, paged_split(B, H, Hkv, max_len).parts) * sizeof(float);
+  return paged_partial_floats(B, H, d, paged_split(B, H, Hkv, max_len).ranges) * sizeof(float);
 }
 
 hipError_t launch_paged_attention(const PagedView& c, int dtype, int B, int H, const void* q, long long q_bytes, const int32_t* kv_len, int max_len,
                                   float scale, void* out, float* lse, void* workspace, hipStream_t st) {
+  const int units = paged_units(H, c.Hkv);
   const PagedSplit s = paged_split(B, H, c.Hkv, max_len);
   float* part_o = (float*)workspace;
-  const AttnArgs a = {c, (const char*)q, q_bytes, kv_len, max_len, H, H / c.Hkv, s.chunk, s.parts, divisor(c.Hkv * s.row_tiles), divisor(c.Hkv),
-                      scale * 1.4426950408889634f, out, lse, part_o, part_o ? part_o + (size_t)B * H * s.parts * c.d : nullptr};
-  const int units = c.Hkv * s.row_tiles;
-  if (dtype == PAGED_FP8) return c.d == 128 ? launch<PAGED_FP8, 128>(a, B, units, st) : launch<PAGED_FP8, 64>(a, B, units, st);
-  if (dtype == PAGED_BF16) return c.d == 128 ? launch<PAGED_BF16, 128>(a, B, units, st) : launch<PAGED_BF16, 64>(a, B, units, st);
-  return c.d == 128 ? launch<PAGED_FP32, 128>(a, B, units, st) : launch<PAGED_FP32, 64>(a, B, units, st);
+  const AttnArgs a = {c, (const char*)q, q_bytes, kv_len, max_len, H, H / c.Hkv, B, units, s.ranges, divisor(units), divisor(c.Hkv),
+                      scale * 1.4426950408889634f, out, lse, part_o, part_o ? part_o + (size_t)(s.ranges + B) * H * c.d : nullptr};
+  if (dtype == PAGED_FP8) return c.d == 128 ? launch<PAGED_FP8, 128>(a, s, st) : launch<PAGED_FP8, 64>(a, s, st);
+  if (dtype == PAGED_BF16) return c.d == 128 ? launch<PAGED_BF16, 128>(a, s, st) : launch<PAGED_BF16, 64>(a, s, st);
+  return c.d == 128 ? launch<PAGED_FP32, 128>(a, s, st) : launch<PAGED_FP32, 64>(a, s, st);
 }

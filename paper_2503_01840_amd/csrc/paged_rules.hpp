@@ -1,23 +1,43 @@
-// Into how many parts the attention of single tokens over pages splits a context (host code).
+// How the attention of single tokens over pages divides its work: the rule by sizes (host code), and the division itself (host and device).
 #pragma once
 #include <algorithm>
 #include <cstddef>
 
-constexpr int PAGED_ROWS = 16;            // query heads of one KV head that a workgroup has
+#include "divisor.hpp"
+
+constexpr int PAGED_ROWS = 16;            // query heads of one KV head that a wavefront has
+constexpr int PAGED_WAVES = 8;            // wavefronts of a workgroup
+
+// (KV head, row tile) pairs of a sequence
+inline int paged_units(int H, int Hkv) { return Hkv * ((H / Hkv + PAGED_ROWS - 1) / PAGED_ROWS); }
 
 struct PagedSplit {
-  int chunk;                              // keys of a part
-  int parts;                              // of the longest context that a launch has to expect
-  int row_tiles;                          // workgroups that a KV head's query heads take
+  int ranges;                             // into how many all sequences' keys are divided; 0: a workgroup per sequence and unit, one launch
+  bool team;                              // a range of a unit to a workgroup, else to a wavefront
 };
-
+// A launch that knows only a bound of the lengths.  Times in us, whole / team / wavefronts, 32 heads of 128 over 8:
+//   A CU draws some 50 GB/s, so a whole context goes to one workgroup where it is short: one sequence of 256 tokens 5.7 / 6.9 / 9.1, of 512
+//   7.8 / 7.6 / 9.7, of 2048 23.5 / 9.6 / 11.6 (bf16); or where sequences fill the chip and a second launch costs more than uneven lengths: 32 of
+//   500..1024 tokens 24.9 / 28.3 / 29.1, 64 of 300..1024 42.9 / 42.1 / 41.9, but of 512..2048 78.7 / 70.3 / 69.5.
+//   A wavefront with a range of its own has no exchange at the end and reads whole rows together with its neighbours, but needs a long range:
+//   64 of 512..2048 in 8 bits 48.7 / 45.8 / 42.0, 131071 tokens in 8 bits under 64 heads 63.1 (team) / 59.6, 256 of 1300 in bf16 259 / 237; 8 of
+//   4000..8192 43.7 / 44.6, 16 of 1000..2048 in fp32 41.9 / 46.2, one of 16384 under 64 heads 20.6 / 24.9.
 inline PagedSplit paged_split(int B, int H, int Hkv, int max_len) {
-  const int tiles = (H / Hkv + PAGED_ROWS - 1) / PAGED_ROWS;
-  const long units = (long)B * Hkv * tiles, target = 2048;
-  const long parts = std::max(1l, std::min((target + units - 1) / units, (max_len + 255l) / 256));
-  const int chunk = (int)(((max_len + parts - 1) / parts + 127) / 128 * 128);
-  return {chunk, (max_len + chunk - 1) / chunk, tiles};
+  const long units = paged_units(H, Hkv), keys = (long)B * max_len;
+  if (max_len <= 512 || (max_len <= 1024 && B * units >= 256) || B > 1024 || keys >= 1l << 33) return {0, false};
+  const bool team = keys * units < 2048l * 384;
+  return {(int)std::max(1l, std::min((team ? 256 : 256 * PAGED_WAVES) / units, keys / 64)), team};
 }
 
-// fp32 elements of the parts' results: D sums, the maximum and the sum of weights, for every head and part
-inline size_t paged_partial_floats(int B, int H, int D, int parts) { return parts > 1 ? (size_t)B * H * parts * (D + 2) : 0; }
+// fp32 elements of the parts' results: D sums, the maximum and the sum of weights, for every head
+inline size_t paged_partial_floats(int B, int H, int D, int ranges) { return ranges > 0 ? (size_t)(ranges + B) * H * (D + 2) : 0; }
+
+// Tiles of a range, of `total`.  Range r has tiles r * per .. (r + 1) * per - 1, counted over all sequences, some ranges none.
+HOST_AND_DEVICE int paged_tiles_of_range(int total, int ranges) {
+  const int per = (int)((total + (long long)ranges - 1) / ranges);
+  return per > 1 ? per : 1;
+}
+// The ranges that a sequence with tiles starts .. ends - 1 lies in.  Its part of range r is kept in place r + b: from one part to the next in the order of the
+// tiles either r or b grows, so that no two share a place, and there are fewer than ranges + B.
+HOST_AND_DEVICE int paged_first_range(int starts, int per) { return starts / per; }
+HOST_AND_DEVICE int paged_last_range(int ends, int per) { return (ends - 1) / per; }

@@ -56,7 +56,7 @@ def _check(c, table, q, lens, got, lse, scale=None):
 
 def _run(dtype, H, Hkv, d, page, lens, seed, max_len=None, q_scale=2.0, scale=None, packed=False):
     g = torch.Generator().manual_seed(seed)
-    max_pages = -(-max(max(lens), 1) // page) + 1
+    max_pages = -(-max(max(lens), max_len or 1) // page) + 1
     c, table = make_cache(dtype, len(lens), max_pages, page, Hkv, d, g)
     if dtype == "fp8":                                       # values of ordinary size: exponents around those of a normal row
         for e in (c.k_exp, c.v_exp):
@@ -120,6 +120,16 @@ def test_bounds_ahead_of_the_lengths(dtype, B, bound):
     _check(c, wide, q, [min(n, 300) if i % 2 else 300 for i, n in enumerate(lens)], out, lse)
     out, lse = E.eagle3_paged_attention(c, q, less, 500, want_lse=True)
     _check(c, wide, q, [0 if n % 3 == 0 else n for n in lens], out, lse)
+
+
+# batches of more than one look at 64 lengths, with idle places: ranges of a workgroup, of a wavefront, and a workgroup to each sequence
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("B,hi", [(65, 1500), (130, 1500), (300, 1500), (1100, 1100)])
+def test_many_ragged_sequences(dtype, B, hi):
+    g = torch.Generator().manual_seed(B)
+    lens = [n if n % 5 else 0 for n in (torch.rand(B, generator=g) ** 3 * hi).int().tolist()]
+    lens[0], lens[63], lens[64], lens[-1] = 0, hi, 1, hi - 1
+    _run(dtype, 4, 2, 64, 16 if B % 2 else 24, lens, B, max_len=hi + 17)
 
 
 def test_scales_and_packed_queries():
