@@ -425,10 +425,13 @@ def _gpu_of(t, what):
     return gpu
 
 
+_raw_stream, _current_gpu = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice       # what torch.cuda's functions ask, 2 us sooner
+
+
 def _on(gpu, call, *args):
     """The call on that GPU's own current stream, whichever GPU is current."""
-    stream = torch._C._cuda_getCurrentRawStream(gpu)
-    if gpu == torch.cuda.current_device():
+    stream = _raw_stream(gpu)
+    if gpu == _current_gpu():
         code = call(*args, stream)
     else:
         with torch.cuda.device(gpu):
@@ -458,6 +461,16 @@ class Rope:
 _ROPE_TYPES = {torch.bfloat16: EAGLE3_BF16, torch.float32: EAGLE3_FP32}
 
 
+def _rotated(x, y, dtype, rows, heads, d, gpu, what):
+    """Addresses and row strides of x and of where it goes: y, or a new dense tensor, which is returned too."""
+    p, stride = _rows_arg(x, dtype, rows, heads, d, gpu, what)
+    if y is None:
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+        return p, stride, y.data_ptr(), x.shape[1] * d, y
+    to, y_stride = _rows_arg(y, dtype, rows, x.shape[1], d, gpu, "out of " + what)
+    return p, stride, to, y_stride, y
+
+
 def _rotate(call, rope, positions, q, k, out):
     gpu, dtype = _gpu_of(q, "q"), q.dtype
     code = _ROPE_TYPES.get(dtype)
@@ -465,22 +478,15 @@ def _rotate(call, rope, positions, q, k, out):
         _refuse("q", f"bf16 or fp32 [rows, heads, d] on cuda:{rope.gpu}", q)
     rows, H, d = q.shape
     pos = _arg(positions, torch.int32, (rows,), gpu, "positions")
-    qp, q_stride = _rows_arg(q, dtype, rows, H, d, gpu, "q")
     q_out, k_out = out if isinstance(out, (tuple, list)) else (out, None)
-    if q_out is None:
-        q_out = torch.empty((rows, H, d), dtype=dtype, device=q.device)
-    qo, qo_stride = _rows_arg(q_out, dtype, rows, H, d, gpu, "out of q")
+    qp, q_stride, qo, qo_stride, q_out = _rotated(q, q_out, dtype, rows, H, d, gpu, "q")
     if k is None:
         if k_out is not None:
             _refuse("out of k", "None without k", k_out)
         _on(gpu, call, code, rows, d, rope.c, pos, H, qp, q_stride, qo, qo_stride, 0, None, 0, None, 0)
         return q_out
-    kp, k_stride = _rows_arg(k, dtype, rows, None, d, gpu, "k")
-    Hkv = k.shape[1]
-    if k_out is None:
-        k_out = torch.empty((rows, Hkv, d), dtype=dtype, device=q.device)
-    ko, ko_stride = _rows_arg(k_out, dtype, rows, Hkv, d, gpu, "out of k")
-    _on(gpu, call, code, rows, d, rope.c, pos, H, qp, q_stride, qo, qo_stride, Hkv, kp, k_stride, ko, ko_stride)
+    kp, k_stride, ko, ko_stride, k_out = _rotated(k, k_out, dtype, rows, None, d, gpu, "k")
+    _on(gpu, call, code, rows, d, rope.c, pos, H, qp, q_stride, qo, qo_stride, k.shape[1], kp, k_stride, ko, ko_stride)
     return q_out, k_out
 
 
@@ -562,13 +568,16 @@ def eagle3_paged_attention(cache, q, kv_len, max_kv_len, scale=None, out=None, w
     qp, stride = _rows_arg(q, dtype, B, None, d, gpu, "q")
     H = q.shape[1]
     if out is None:
-        out = torch.empty((B, H, d), dtype=dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        to = out.data_ptr()
+    else:
+        to = _arg(out, dtype, (B, H, d), gpu, "out")
     lse = torch.empty((B, H), dtype=torch.float32, device=q.device) if want_lse else None
     need = C.c_size_t()
     _check(L.eagle3_paged_attention_workspace(cache.c, B, H, max_kv_len, need))
     need = need.value
     ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     _on(gpu, L.eagle3_paged_attention, cache.c, B, H, qp, stride, _arg(kv_len, torch.int32, (B,), gpu, "kv_len"), max_kv_len,
-        d ** -0.5 if scale is None else scale, _arg(out, dtype, (B, H, d), gpu, "out"), None if lse is None else lse.data_ptr(),
+        d ** -0.5 if scale is None else scale, to, None if lse is None else lse.data_ptr(),
         None if ws is None else ws.data_ptr(), need)
     return (out, lse) if want_lse else out

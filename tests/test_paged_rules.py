@@ -46,7 +46,7 @@ int main() {
           NEED(units == Hkv * ((G + 15) / 16));
           NEED(ranges >= 0 && ranges <= 256 * PAGED_WAVES);
           NEED(ranges == 0 || ((long)B * (n / 16 + 1) < 1l << 30 && B <= 1024 && (long)ranges * units <= std::max(256l * PAGED_WAVES, (long)units)));
-          NEED(n > 512 || ranges == 0);
+          NEED(n > 768 || ranges == 0);
         }
   const PagedSplit a = paged_split(1, 32, 8, 4096), b = paged_split(1, 64, 8, 131072), c = paged_split(64, 32, 8, 2048), d = paged_split(64, 32, 8, 1024);
   printf("%d %d  %d %d  %d %d  %d\\n", a.ranges, a.team, b.ranges, b.team, c.ranges, c.team, d.ranges);
