@@ -471,13 +471,27 @@ __global__ __launch_bounds__(64 * WAVES) void paged_ranges_kernel(AttnArgs p) {
   }
 }
 
-// The parts of a (sequence, query head), D / 4 lanes to each, JW wavefronts to a head; and the sequences without a token.
-template <int KEYS, bool F32, int D, int JW>
+// What is joined: a maximum, a sum of weights and four sums of values.
+struct Joint {
+  float M, L;
+  floatx4 sum;
+  __device__ __forceinline__ void add(float m, float l, const floatx4& v) {
+    const float to = fmaxf(M, m), a = exp2_fast(M - to), c = exp2_fast(m - to);
+    M = to;
+    L = L * a + l * c;
+    sum = sum * a + v * c;
+  }
+};
+
+// The parts of a (sequence, query head), and the sequences without a token.  DL lanes have DL * 4 dimensions of a part, a head's WAVES_PER wavefronts as many
+// parts at a time as they have such groups, four of them in flight; groups are joined by exchanges within a wavefront, then through LDS.
+// Few parts: a wavefront to a head with all its dimensions.  Many (131072 tokens under 64 heads: 256 parts): eight, with 32 dimensions, 8.1 -> 5.8 us.
+template <int KEYS, bool F32, int D, int DL, int WAVES_PER>
 __global__ __launch_bounds__(512) void paged_join_kernel(AttnArgs p) {
-  constexpr int LANES = D / 4, PER = 64 * JW / LANES, HEADS = 8 / JW;
-  __shared__ __attribute__((aligned(16))) float so[HEADS][PER][D], sml[HEADS][PER][2];
-  const int mine = threadIdx.x / (64 * JW), h = blockIdx.x * HEADS + mine, b = blockIdx.y, n = length_of(p, b);
-  const int at = threadIdx.x % (64 * JW) / LANES, d = threadIdx.x % LANES * 4;
+  constexpr int PER = 64 * WAVES_PER / DL, HEADS = 8 / WAVES_PER;
+  __shared__ __attribute__((aligned(16))) float so[8][4 * DL], sml[8][2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.x * HEADS + wave / WAVES_PER, b = blockIdx.y, n = length_of(p, b);
+  const int at = threadIdx.x % (64 * WAVES_PER) / DL, d = blockIdx.z * (4 * DL) + lane % DL * 4;
   int total = 0, ends = 0;
   for (int b0 = 0; b0 < p.B; b0 += 64) {
     const int scanned = scan_tiles<KEYS>(p, b0);
@@ -488,41 +502,39 @@ __global__ __launch_bounds__(512) void paged_join_kernel(AttnArgs p) {
     if (at == 0 && h < p.H) store_nothing<F32, D>(p, b, h, d);
     return;
   }
-  const int per = paged_tiles_of_range(total, p.ranges), starts = ends - (n + KEYS - 1) / KEYS, first = paged_first_range(starts, per), parts = paged_last_range(ends, per) - first + 1;
+  const int per = paged_tiles_of_range(total, p.ranges), starts = ends - (n + KEYS - 1) / KEYS;
+  const int first = paged_first_range(starts, per), parts = paged_last_range(ends, per) - first + 1;
   if (parts <= 1) return;
   const size_t part0 = (size_t)(first + b) * p.H + min(h, p.H - 1);
-  float M = -FLT_MAX, L = 0.f;
-  floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = at; i0 < parts; i0 += 4 * PER) {              // four parts in flight
+  Joint j = {-FLT_MAX, 0.f, {0.f, 0.f, 0.f, 0.f}};
+  for (int i0 = at; i0 < parts; i0 += 4 * PER) {
     float2 ml[4];
     floatx4 v[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const size_t part = part0 + (size_t)min(i0 + j * PER, parts - 1) * p.H;
-      ml[j] = *(const float2*)(p.part_ml + part * 2);
-      v[j] = *(const floatx4*)(p.part_o + part * D + d);
+    for (int i = 0; i < 4; ++i) {
+      const size_t part = part0 + (size_t)min(i0 + i * PER, parts - 1) * p.H;
+      ml[i] = *(const float2*)(p.part_ml + part * 2);
+      v[i] = *(const floatx4*)(p.part_o + part * D + d);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (i0 + j * PER < parts) {
-        const float to = fmaxf(M, ml[j].x), a = exp2_fast(M - to), c = exp2_fast(ml[j].x - to);
-        M = to;
-        L = L * a + ml[j].y * c;
-        sum = sum * a + v[j] * c;
-      }
+    for (int i = 0; i < 4; ++i)
+      if (i0 + i * PER < parts) j.add(ml[i].x, ml[i].y, v[i]);
+  }
+#pragma unroll
+  for (int o = DL; o < 64; o *= 2) {
+    const float m = __shfl_xor(j.M, o, 64), l = __shfl_xor(j.L, o, 64);
+    j.add(m, l, floatx4{__shfl_xor(j.sum[0], o, 64), __shfl_xor(j.sum[1], o, 64), __shfl_xor(j.sum[2], o, 64), __shfl_xor(j.sum[3], o, 64)});
+  }
+  if constexpr (WAVES_PER > 1) {
+    if (lane < DL) {
+      *(floatx4*)&so[wave][4 * lane] = j.sum;
+      if (lane == 0) { sml[wave][0] = j.M; sml[wave][1] = j.L; }
     }
+    __syncthreads();
+    if (threadIdx.x >= DL) return;
+    for (int i = 1; i < WAVES_PER; ++i) j.add(sml[i][0], sml[i][1], *(const floatx4*)&so[i][4 * lane]);
   }
-  *(floatx4*)&so[mine][at][d] = sum;
-  if (d == 0) { sml[mine][at][0] = M; sml[mine][at][1] = L; }
-  __syncthreads();
-  if (at > 0 || h >= p.H) return;
-  for (int i = 1; i < min(PER, parts); ++i) {
-    const float to = fmaxf(M, sml[mine][i][0]), a = exp2_fast(M - to), c = exp2_fast(sml[mine][i][0] - to);
-    M = to;
-    L = L * a + sml[mine][i][1] * c;
-    sum = sum * a + *(const floatx4*)&so[mine][i][d] * c;
-  }
-  store_result<F32, D>(p, b, h, d, sum, M, L);
+  if (lane < DL && h < p.H) store_result<F32, D>(p, b, h, d, j.sum, j.M, j.L);
 }
 
 template <int TYPE, int D, bool BLOCKED>
@@ -536,8 +548,8 @@ hipError_t launch(const AttnArgs& a, const PagedSplit& s, hipStream_t st) {
   else hipLaunchKernelGGL((paged_ranges_kernel<TYPE, D, BLOCKED, false>), dim3((n + WAVES - 1) / WAVES), dim3(64 * WAVES), 0, st, a);
   constexpr int KEYS = 16 * CacheType<TYPE>::BLOCKS;
   constexpr bool F32 = TYPE == PAGED_FP32;
-  if (s.ranges / a.B > 16) hipLaunchKernelGGL((paged_join_kernel<KEYS, F32, D, 8>), dim3(a.H, a.B), dim3(512), 0, st, a);
-  else hipLaunchKernelGGL((paged_join_kernel<KEYS, F32, D, 1>), dim3((a.H + 7) / 8, a.B), dim3(512), 0, st, a);
+  if (s.ranges / a.B > 16) hipLaunchKernelGGL((paged_join_kernel<KEYS, F32, D, 8, 8>), dim3(a.H, a.B, D / 32), dim3(512), 0, st, a);
+  else hipLaunchKernelGGL((paged_join_kernel<KEYS, F32, D, D / 4, 1>), dim3((a.H + 7) / 8, a.B), dim3(512), 0, st, a);
   return hipGetLastError();
 }
 template <int TYPE, int D>

@@ -17,7 +17,7 @@ struct PagedSplit {
 };
 // A launch that knows only a bound of the lengths.  Times in us, whole / team / wavefronts, 32 heads of 128 over 8:
 //   A CU draws some 50 GB/s, so a whole context goes to one workgroup where it is short: one sequence of 256 tokens 5.7 / 6.9 / 9.1, of 512
-//   7.8 / 7.1 / 9.7, of 768 10.0 / 8.8 / 10.5, of 2048 23.5 / 9.7 / 11.6 (bf16).  The second launch that parts need costs the host 4 us more, so up to 768;
+//   7.8 / 7.1 / 9.7, of 768 10.8 / 8.2 / 10.5, of 2048 23.5 / 9.7 / 11.6 (bf16).  The second launch that parts need costs the host 4 us more, so up to 768;
 //   and where sequences fill the chip it costs more than uneven lengths: 32 of 500..1024 tokens 24.9 / 28.3 / 29.1, 64 of 300..1024 42.9 / 42.1 / 41.9, but
 //   of 512..2048 78.7 / 70.3 / 69.5.
 //   A wavefront with a range of its own has no exchange at the end and reads whole rows together with its neighbours, but needs a long range:
