@@ -321,7 +321,7 @@ int eagle3_rope_grad(int32_t dtype, int32_t rows, int32_t head_dim, const eagle3
 typedef struct {
   void *k, *v;                            /* DEVICE [n_pages, page_size, n_kv_heads, head_dim], at multiples of 16 bytes       */
   uint8_t *k_exp, *v_exp;                 /* DEVICE [n_pages, page_size, n_kv_heads]; EAGLE3_FP8 only, else NULL               */
-  const int32_t* page_table;              /* DEVICE [B, max_pages]; entries behind a sequence's last page are not read        */
+  const int32_t* page_table;              /* DEVICE [B, max_pages]; what stands behind a sequence's last page has no effect   */
   int32_t dtype;                          /* EAGLE3_BF16, EAGLE3_FP32 or EAGLE3_FP8                                            */
   int32_t n_pages, page_size, max_pages;  /* any sizes >= 1 with n_pages * page_size and max_pages * page_size < 2^31          */
   int32_t n_kv_heads, head_dim;           /* head_dim 64 or 128                                                                */
@@ -356,7 +356,7 @@ int eagle3_paged_read(const eagle3_paged_kv* kv, int32_t B, int32_t rows, const 
  *              multiples of 16 bytes; query head h reads KV head h * n_kv_heads / n_heads
  *   kv_len     DEVICE int32 [B], clamped to 0..max_kv_len; 0: out = 0, lse = -infinity
  *   max_kv_len HOST bound >= 1, at most max_pages * page_size and 2^30; sizes the launch
- *   out        [B, n_heads, head_dim], dense, of q's type; lse fp32 [B, n_heads] or NULL
+ *   out        [B, n_heads, head_dim], dense, of q's type, apart from q; lse fp32 [B, n_heads] or NULL
  *   workspace  DEVICE, 256-byte aligned, of the bytes that the next call tells for the same sizes; NULL if these are 0.  Its content
  *              need not be kept or cleared between calls; calls that may overlap in time need one each.
  * Page numbers are clamped into the pool.  A sequence's infinite or NaN keys and values make its results NaN or infinite, no other's.

@@ -867,7 +867,7 @@ int eagle3_paged_attention_workspace(const eagle3_paged_kv* kv, int32_t B, int32
   if (!bytes) return EAGLE3_E_NULL;
   PagedView c;
   TRY(paged_attention_sizes(kv, B, n_heads, max_kv_len, c));
-  *bytes = paged_attention_workspace(B, n_heads, c.Hkv, c.d, max_kv_len);
+  *bytes = paged_attention_workspace(c, kv->dtype, B, n_heads, max_kv_len);
   return EAGLE3_OK;
 }
 
@@ -880,7 +880,7 @@ int eagle3_paged_attention(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads
   const int64_t size = kv->dtype == EAGLE3_FP32 ? 4 : 2;
   if (q_stride < (int64_t)n_heads * c.d || q_stride > INT64_MAX / 4 / B || q_stride * size % 16 || (((uintptr_t)q | (uintptr_t)out) & 15))
     return EAGLE3_E_SHAPE;
-  const size_t need = paged_attention_workspace(B, n_heads, c.Hkv, c.d, max_kv_len);
+  const size_t need = paged_attention_workspace(c, kv->dtype, B, n_heads, max_kv_len);
   if (need > workspace_bytes || (need && (!workspace || ((uintptr_t)workspace & 255)))) return EAGLE3_E_STATE;
   CK(launch_paged_attention(c, kv->dtype, B, n_heads, q, q_stride * size, kv_len, max_kv_len, scale, out, lse, workspace, (hipStream_t)stream));
   return EAGLE3_OK;

@@ -237,6 +237,6 @@ struct PagedView;
 // Rows of B sequences to (read: from) their slots; dense rows row_bytes apart.
 hipError_t launch_paged_rows(const PagedView& c, int dtype, bool read, int B, int rows, const int32_t* start, const int32_t* n,
                              const int32_t* row_start, void* k, void* v, long long n_rows, long long row_bytes, hipStream_t st);
-size_t paged_attention_workspace(int B, int H, int Hkv, int d, int max_len);
+size_t paged_attention_workspace(const PagedView& c, int dtype, int B, int H, int max_len);
 hipError_t launch_paged_attention(const PagedView& c, int dtype, int B, int H, const void* q, long long q_bytes, const int32_t* kv_len, int max_len,
                                   float scale, void* out, float* lse, void* workspace, hipStream_t st);

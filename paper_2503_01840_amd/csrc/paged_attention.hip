@@ -400,11 +400,33 @@ __device__ __forceinline__ void store_nothing(const AttnArgs& p, int b, int h, i
   if (d == 0 && p.lse != nullptr) p.lse[bh] = -__builtin_huge_valf();
 }
 
-// Short contexts: a workgroup per sequence and unit; one launch.
+// The sequence in place `at` when of every 64, those behind the last whole 64 before the others, the longest comes first: every lane counts the longer ones for its
+// sequence, a wavefront an eighth of them.
+__device__ __forceinline__ int longest_first(const AttnArgs& p, int wave, int at) {
+  __shared__ int ranks[WAVES][64];
+  const int lane = threadIdx.x & 63, rest = p.B & 63, b0 = at < rest ? p.B - rest : (at - rest) & ~63, place = at < rest ? at : (at - rest) & 63;
+  const long long key = b0 + lane < p.B ? (long long)length_of(p, b0 + lane) * 64 + 63 - lane : -1ll - lane;
+  const int hi = (int)(key >> 32), lo = (int)key;
+  int rank = 0;
+#pragma unroll
+  for (int j = 0; j < 64 / WAVES; ++j) {
+    const long long other = (long long)__builtin_amdgcn_readlane(hi, wave * (64 / WAVES) + j) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, wave * (64 / WAVES) + j);
+    rank += other > key ? 1 : 0;
+  }
+  ranks[wave][lane] = rank;
+  __syncthreads();
+  rank = 0;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) rank += ranks[i][lane];
+  return b0 + __builtin_ctzll(__ballot(rank == place));
+}
+
+// Short contexts, or very many: a workgroup per sequence and unit; one launch.  Where there are more workgroups than CUs, those of long sequences
+// begin first: 64 of 512..2048 tokens, 32 heads over 8, bf16 76.6 -> 65.2 us.
 template <int TYPE, int D, bool BLOCKED>
 __global__ __launch_bounds__(64 * WAVES) void paged_whole_kernel(AttnArgs p) {
   typedef Walk<TYPE, D, BLOCKED> W;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = blockIdx.y;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = p.B > 1 && p.B * p.units > 256 ? longest_first(p, wave, blockIdx.y) : (int)blockIdx.y;
   W w(p);
   w.begin(b, blockIdx.x);
   w.template ask<WAVES>(wave);
@@ -559,14 +581,16 @@ hipError_t launch(const AttnArgs& a, const PagedSplit& s, hipStream_t st) {
 
 }  // namespace
 
-size_t paged_attention_workspace(int B, int H, int Hkv, int d, int max_len) {
-  return paged_partial_floats(B, H, d, paged_split(B, H, Hkv, max_len).ranges) * sizeof(float);
+static int cached_row_bytes(const PagedView& c, int dtype) { return c.d * (dtype == PAGED_FP32 ? 4 : dtype == PAGED_BF16 ? 2 : 1); }
+
+size_t paged_attention_workspace(const PagedView& c, int dtype, int B, int H, int max_len) {
+  return paged_partial_floats(B, H, c.d, paged_split(B, H, c.Hkv, cached_row_bytes(c, dtype), max_len).ranges) * sizeof(float);
 }
 
 hipError_t launch_paged_attention(const PagedView& c, int dtype, int B, int H, const void* q, long long q_bytes, const int32_t* kv_len, int max_len,
                                   float scale, void* out, float* lse, void* workspace, hipStream_t st) {
   const int units = paged_units(H, c.Hkv);
-  const PagedSplit s = paged_split(B, H, c.Hkv, max_len);
+  const PagedSplit s = paged_split(B, H, c.Hkv, cached_row_bytes(c, dtype), max_len);
   float* part_o = (float*)workspace;
   const AttnArgs a = {c, (const char*)q, q_bytes, kv_len, max_len, H, H / c.Hkv, B, units, s.ranges, divisor(units), divisor(c.Hkv),
                       scale * 1.4426950408889634f, out, lse, part_o, part_o ? part_o + (size_t)(s.ranges + B) * H * c.d : nullptr};

@@ -17,15 +17,18 @@ struct PagedSplit {
 };
 // A launch that knows only a bound of the lengths.  Times in us, whole / team / wavefronts, 32 heads of 128 over 8:
 //   A CU draws some 50 GB/s, so a whole context goes to one workgroup where it is short: one sequence of 256 tokens 5.7 / 6.9 / 9.1, of 512
-//   7.8 / 7.1 / 9.7, of 768 10.8 / 8.2 / 10.5, of 2048 23.5 / 9.7 / 11.6 (bf16).  The second launch that parts need costs the host 4 us more, so up to 768;
-//   and where sequences fill the chip it costs more than uneven lengths: 32 of 500..1024 tokens 24.9 / 28.3 / 29.1, 64 of 300..1024 42.9 / 42.1 / 41.9, but
-//   of 512..2048 78.7 / 70.3 / 69.5.
+//   7.8 / 7.1 / 9.7, of 768 10.8 / 8.2 / 10.5, of 2048 23.5 / 9.7 / 11.6 (bf16).  The second launch that parts need costs the host 4 us more, so up to 768.
+//   Where sequences fill the chip (the longest begin first) the second launch costs more than uneven lengths: 32 of 500..1024 tokens 24.9 / 28.3 / 29.1, 64 of
+//   300..1024 38.1 / 42.9 / 42.5, 48 of 512..2048 53.6 / 56.0 / 55.8, 64 of them 65.2 / 70.1 / 69.4, in fp32 117 / 120 / 128; but 32 of 500..4096 75.2 / 64.5 / 62.8,
+//   and where a head's row is one memory line only, 64 of 512..2048 in 8 bits 45.9 / 45.9 / 42.0, in bf16 with 64 dimensions 43.3 / 44.7 / 37.8.
 //   A wavefront with a range of its own has no exchange at the end and reads whole rows together with its neighbours, but needs a long range:
-//   64 of 512..2048 in 8 bits 48.7 / 45.8 / 42.0, 131071 tokens in 8 bits under 64 heads 63.1 (team) / 59.6, 256 of 1300 in bf16 259 / 237; 8 of
-//   4000..8192 43.7 / 44.6, 16 of 1000..2048 in fp32 41.9 / 46.2, one of 16384 under 64 heads 20.6 / 24.9.
-inline PagedSplit paged_split(int B, int H, int Hkv, int max_len) {
-  const long units = paged_units(H, Hkv), keys = (long)B * max_len;
-  if (max_len <= 768 || (max_len <= 1024 && B * units >= 256) || B > 1024 || keys >= 1l << 33) return {0, false};
+//   131071 tokens in 8 bits under 64 heads 62.4 (team) / 57.3, 256 of 1300 in bf16 259 / 237; 8 of 4000..8192 44.6 / 45.1, 16 of 1000..2048 in fp32
+//   41.9 / 46.2, one of 16384 under 64 heads 19.8 / 22.7.
+// row_bytes: of a head's row in the cache.
+inline PagedSplit paged_split(int B, int H, int Hkv, int row_bytes, int max_len) {
+  const long units = paged_units(H, Hkv), keys = (long)B * max_len, groups = B * units;
+  if (max_len <= 768 || (max_len <= 1024 && groups >= 256) || (max_len <= 2048 && groups >= 320 && row_bytes >= 256)) return {0, false};
+  if (B > 1024 || keys >= 1l << 33) return {0, false};       // what a wavefront looks through, and counts in 32 bits
   const bool team = keys * units < 2048l * 384;
   return {(int)std::max(1l, std::min((team ? 256 : 256 * PAGED_WAVES) / units, keys / 64)), team};
 }

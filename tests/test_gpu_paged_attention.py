@@ -122,6 +122,13 @@ def test_bounds_ahead_of_the_lengths(dtype, B, bound):
     _check(c, wide, q, [0 if n % 3 == 0 else n for n in lens], out, lse)
 
 
+# enough keys for a range to every wavefront, in pages of whole blocks of 16 keys and in others
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("page", [48, 20])
+def test_ranges_of_wavefronts(dtype, page):
+    _run(dtype, 16, 16, 64, page, [26000, 0, 25011], page)
+
+
 # batches of more than one look at 64 lengths, with idle places: ranges of a workgroup, of a wavefront, and a workgroup to each sequence
 @pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
 @pytest.mark.parametrize("B,hi", [(65, 1500), (130, 1500), (300, 1500), (1100, 1100)])
@@ -286,6 +293,22 @@ def test_two_streams_at_once():
                 got[i].append(E.eagle3_paged_attention(c, (q, q2)[i], n, 3000))
     torch.cuda.synchronize()
     assert all(torch.equal(t, out) for t in got[0]) and all(torch.equal(t, want) for t in got[1])
+
+
+def test_calls_go_to_the_tensors_gpu(monkeypatch):
+    """With another GPU current the call changes over to the tensors' own and back (one GPU here: the current one's number is what is pretended)."""
+    from paper_2503_01840_amd import binding as Bd
+    c, table, q, n, out, _ = _run("bf16", 8, 2, 128, 16, [100, 200], 40)
+    seen = []
+    real = torch.cuda.device
+
+    class Device(real):
+        def __init__(self, d):
+            seen.append(d)
+            super().__init__(d)
+    monkeypatch.setattr(Bd, "_current_gpu", lambda: 5)
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    assert torch.equal(E.eagle3_paged_attention(c, q, n, 200), out) and seen == [q.device.index]
 
 
 def test_binding_refuses_what_does_not_fit():

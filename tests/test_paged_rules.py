@@ -41,14 +41,14 @@ int main() {
       for (int G : {1, 4, 16, 17, 64})
         for (int n : {1, 511, 512, 513, 1024, 1025, 4096, 131072, 1 << 30}) {
           const int H = Hkv * G, units = paged_units(H, Hkv), total = 0;
-          const PagedSplit s = paged_split(B, H, Hkv, n);
+          const PagedSplit s = paged_split(B, H, Hkv, 128 << (B & 1), n);
           const int ranges = s.ranges;
           NEED(units == Hkv * ((G + 15) / 16));
           NEED(ranges >= 0 && ranges <= 256 * PAGED_WAVES);
           NEED(ranges == 0 || ((long)B * (n / 16 + 1) < 1l << 30 && B <= 1024 && (long)ranges * units <= std::max(256l * PAGED_WAVES, (long)units)));
           NEED(n > 768 || ranges == 0);
         }
-  const PagedSplit a = paged_split(1, 32, 8, 4096), b = paged_split(1, 64, 8, 131072), c = paged_split(64, 32, 8, 2048), d = paged_split(64, 32, 8, 1024);
+  const PagedSplit a = paged_split(1, 32, 8, 256, 4096), b = paged_split(1, 64, 8, 128, 131072), c = paged_split(64, 32, 8, 128, 2048), d = paged_split(64, 32, 8, 256, 2048);
   printf("%d %d  %d %d  %d %d  %d\\n", a.ranges, a.team, b.ranges, b.team, c.ranges, c.team, d.ranges);
   return 0;
 }
