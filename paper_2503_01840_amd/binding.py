@@ -415,7 +415,7 @@ def _rows_arg(t, dtype, rows, heads, d, gpu, what):
         ok = (rows is None or n == rows) and (heads is None or h == heads) and m == d and s2 == 1 and (s1 == d or h == 1) and (s0 >= h * d or n <= 1)
     if not ok:
         _refuse(what, f"{dtype} rows [{rows}, {heads}, {d}], each with its heads one behind the other, on cuda:{gpu}", t)
-    return t.data_ptr(), s0 if s0 > h * d else h * d
+    return t.data_ptr(), s0 if n > 1 else h * d
 
 
 def _gpu_of(t, what):
