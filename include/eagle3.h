@@ -303,7 +303,7 @@ int eagle3_rope_turns(int32_t rot_dim, double theta, int32_t scaling, double fac
  *   q, k        row r's heads [n_heads, head_dim] at q + r * q_stride elements (k likewise): q_stride >= n_heads * head_dim, so that
  *               they may be parts of longer rows such as those of a joint q|k|v product
  *   q_out       the same with a stride of its own; q_out == q with equal strides rotates in place, other overlaps are not allowed
- * Requires 1 <= rows <= 2^30, n_heads, n_kv_heads >= 1, even head_dim <= 1024, (n_heads + n_kv_heads) * head_dim < 2^30 and, times rows, < 2^40. */
+ * Requires 1 <= rows < 2^24, n_heads, n_kv_heads >= 1, even head_dim <= 1024, (n_heads + n_kv_heads) * head_dim < 2^30 and, times rows, < 2^40. */
 int eagle3_rope(int32_t dtype, int32_t rows, int32_t head_dim, const eagle3_rope_spec* rope, const int32_t* positions, int32_t n_heads,
                 const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int32_t n_kv_heads, const void* k, int64_t k_stride,
                 void* k_out, int64_t k_out_stride, eagle3_stream stream);

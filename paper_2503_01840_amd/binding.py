@@ -492,7 +492,7 @@ def _rotate(call, rope, positions, q, k, out):
 
 def eagle3_rope(rope, positions, q, k=None, out=None):
     """q [rows, H, d] and k [rows, Hkv, d] (bf16 or fp32, rows any distance apart) turned to their positions (int32 [rows]).  `out`: where
-    to, e.g. (q, k) themselves; returns the rotated q, or (q, k)."""
+    to, e.g. (q, k) themselves; returns the rotated q, or (q, k).  Nothing is recorded for autograd: eagle3_rope_grad is its backward pass."""
     return _rotate(lib().eagle3_rope, rope, positions, q, k, out)
 
 

@@ -790,7 +790,7 @@ static int rope_rows(int32_t dtype, int32_t rows, int32_t d, const eagle3_rope_s
                      const RopeTensor& k, float sign, eagle3_stream stream) {
   if (!rope || !rope->turns || !positions || !q.x || !q.y || (k.x && !k.y)) return EAGLE3_E_NULL;
   if (dtype != EAGLE3_BF16 && dtype != EAGLE3_FP32) return EAGLE3_E_SHAPE;
-  if (rows < 1 || rows > 1 << 30 || d < 2 || d > 1024 || d % 2 || rope->rot_dim < 2 || rope->rot_dim > d || rope->rot_dim % 2) return EAGLE3_E_SHAPE;
+  if (rows < 1 || rows >= 1 << 24 || d < 2 || d > 1024 || d % 2 || rope->rot_dim < 2 || rope->rot_dim > d || rope->rot_dim % 2) return EAGLE3_E_SHAPE;
   const RopeTensor* tensors[2] = {&q, &k};
   for (const RopeTensor* t : tensors) {
     if (!t->x) continue;

@@ -215,11 +215,12 @@ struct Walk {
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i) {
       floatx4 s = {0.f, 0.f, 0.f, 0.f};
+      floatx4 part[4] = {s, s, s, s};     // fp32: four sums of a quarter of the products each, for shorter chains of roundings and of instructions
 #pragma unroll
       for (int j = 0; j < T::KL; ++j) {
         if constexpr (F32) {
 #pragma unroll
-          for (int h = 0; h < 4; ++h) s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[i][j][h]), __uint_as_float(q[j][h]), s, 0, 0, 0);
+          for (int h = 0; h < 4; ++h) part[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[i][j][h]), __uint_as_float(q[j][h]), part[h], 0, 0, 0);
         } else if constexpr (FP8) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -232,6 +233,7 @@ struct Walk {
           s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[i][j]), __builtin_bit_cast(bf16x8, q[j]), s, 0, 0, 0);
         }
       }
+      if constexpr (F32) s = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[4 * i + r] = s[r] * p.scale_log2;
     }

@@ -68,8 +68,8 @@ def test_rope_and_gradient_follow_the_formula(case, dtype):
         got = call(rope, p, q, k)
         _check(got[0], q, args, pos, sign)
         _check(got[1], k, args, pos, sign)
-        alone = call(rope, p, q)
-        assert torch.equal(alone, got[0])
+        alone, into = call(rope, p, q), torch.zeros_like(q)
+        assert torch.equal(alone, got[0]) and call(rope, p, q, out=into) is into and torch.equal(into, alone)
     assert torch.equal(q, keep[0]) and torch.equal(k, keep[1])
     # parts of longer rows, in place: the same bits, and the rest of the rows as it was
     both = torch.randn(rows, H + 2 * Hkv, d, generator=g).to(dtype).to(DEV)
@@ -126,6 +126,36 @@ def test_gradient_against_differences(inter):
     # each rotated value is off by 7 units of 2^-24 of its pair (|pair| < 1.25 * 2 * 5 * 2), x + e by half a unit of 8; weights below 5
     bound = H * d * 5 * (2 * 7 * 2.0 ** -24 * 1.25 * 20 + 1.25 * 2 * 2.0 ** -24 * 8 + 7 * 2.0 ** -24 * 1.25 * 10)
     assert float((left - right).abs().max()) <= bound < 0.1 * float(left.abs().max())
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_gradient_as_a_backward_pass(inter):
+    """In a torch.autograd.Function: the gradients that torch finds for the same formula in elementary operations."""
+    rows, H, Hkv, d, rot = 9, 4, 2, 64, 64
+    g = torch.Generator().manual_seed(6)
+    rope = E.Rope(rot, 1e4, interleaved=inter, amplitude=1.5, device=DEV)
+    pos = torch.randint(0, 4096, (rows,), generator=g, dtype=torch.int32).to(DEV)
+
+    class Rotate(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k):
+            return E.eagle3_rope(rope, pos, q, k)
+
+        @staticmethod
+        def backward(ctx, dq, dk):
+            return E.eagle3_rope_grad(rope, pos, dq.contiguous(), dk.contiguous())
+
+    leaves = [torch.randn(rows, h, d, generator=g).to(DEV).requires_grad_() for h in (H, Hkv)]
+    w = [torch.randn(rows, h, d, generator=g).to(DEV) for h in (H, Hkv)]
+    (sum((a * b).sum() for a, b in zip(Rotate.apply(*leaves), w))).backward()
+    t = pos.double()[:, None, None] * 1e4 ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=DEV) / rot)
+    for x, weight in zip(leaves, w):
+        y = x.detach().double().requires_grad_()
+        a, b = (y[..., 0::2], y[..., 1::2]) if inter else (y[..., :rot // 2], y[..., rot // 2:])
+        ra, rb = 1.5 * (a * t.cos() - b * t.sin()), 1.5 * (b * t.cos() + a * t.sin())
+        wa, wb = (weight[..., 0::2], weight[..., 1::2]) if inter else (weight[..., :rot // 2], weight[..., rot // 2:])
+        (ra * wa + rb * wb).sum().backward()
+        assert bool(((x.grad - y.grad).abs() <= 7 * 2.0 ** -24 * 1.5 * 2 * float(weight.abs().max())).all())
 
 
 def test_nan_and_infinity_stay_in_their_pair():
