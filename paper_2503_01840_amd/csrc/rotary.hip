@@ -31,54 +31,38 @@ __device__ __forceinline__ void turn(float xa, float xb, float c, float s, float
   yb = fmaf(xb, c, xa * s);
 }
 
-// Any sizes and addresses: one workgroup per row, one pair or unrotated dimension per thread and round.
-template <typename T>
-__global__ __launch_bounds__(256) void rope_any_kernel(RopeTensor q, RopeTensor k, RopeAngles a, int d) {
-  __shared__ float cs[MAX_PAIRS], sn[MAX_PAIRS];
-  const int r = blockIdx.x, half = a.rot >> 1;
-  const double pos = (double)a.positions[r];
-  for (int i = threadIdx.x; i < half; i += 256) angle(a, pos, i, cs, sn);
-  __syncthreads();
-  const int per_head = half + d - a.rot;            // pairs, then dimensions that stay
-  for (int u = threadIdx.x; u < (q.heads + k.heads) * per_head; u += 256) {
-    const int h = u / per_head, i = u % per_head;
-    const bool is_k = h >= q.heads;
-    const RopeTensor& t = is_k ? k : q;
-    const T* x = (const T*)t.x + (size_t)r * t.stride + (size_t)(is_k ? h - q.heads : h) * d;
-    T* y = (T*)t.y + (size_t)r * t.y_stride + (size_t)(is_k ? h - q.heads : h) * d;
-    if (i < half) {
-      const int ia = a.interleaved ? 2 * i : i, ib = a.interleaved ? 2 * i + 1 : i + half;
-      const float xa = load_f32(x, ia), xb = load_f32(x, ib);
-      float ya, yb;
-      turn(xa, xb, cs[i], sn[i], ya, yb);
-      store_from_f32(y, ia, ya);
-      store_from_f32(y, ib, yb);
+// N elements, as one load or store
+template <int BYTES> struct Bits;
+template <> struct Bits<2> { typedef uint16_t type; };
+template <> struct Bits<4> { typedef uint32_t type; };
+template <> struct Bits<16> { typedef u32x4 type; };
+template <typename T, int N> struct Piece {
+  typename Bits<N * sizeof(T)>::type w;
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (N == 1) return load_f32((const T*)&w, 0);
+    else if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
+  __device__ __forceinline__ void set(const float* f) {
+    if constexpr (N == 1) {
+      store_from_f32((T*)&w, 0, f[0]);
     } else {
-      y[i + half] = x[i + half];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f[i]);
+        else w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+      }
     }
   }
-}
+};
 
-template <typename T> struct Piece { static constexpr int N = 16 / sizeof(T); };
-template <typename T> __device__ __forceinline__ float at(const u32x4& w, int i) {
-  if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
-  else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
-}
-template <typename T> __device__ __forceinline__ u32x4 piece_of(const float* f) {
-  u32x4 w;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f[i]);
-    else w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
-  }
-  return w;
-}
-
-// Everything in whole 16-byte pieces.  per_head: tasks of a head, the first `turning` of them to be rotated (two pieces each in the half layout);
-// tasks of a row go over `share` wavefronts (gridDim.y).
-template <typename T, bool INTERLEAVED>
-__global__ __launch_bounds__(256) void rope_kernel(RopeTensor q, RopeTensor k, RopeAngles a, int rows, int d, Divisor per_head, int turning, int share) {
-  constexpr int N = Piece<T>::N, U = 4;
+// A task is a piece of a head, the first `turning` ones to be rotated.  N > 1: pieces of 16 bytes; neighbours as pairs within a piece (INSIDE), else with the piece
+// `apart` elements on.  N = 1, for any sizes and addresses: the first element of a pair, `step` elements behind the one of the task before.  Tasks of a row go over
+// `share` each of gridDim.y wavefronts.
+template <typename T, int N, bool INSIDE>
+__global__ __launch_bounds__(256) void rope_kernel(RopeTensor q, RopeTensor k, RopeAngles a, int rows, int d, Divisor per_head, int turning, int apart, int step, int share) {
+  constexpr int U = N == 1 ? 8 : 4;
+  typedef Piece<T, N> P;
   __shared__ __attribute__((aligned(16))) float cs[4][MAX_PAIRS], sn[4][MAX_PAIRS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = blockIdx.x * 4 + wave, half = a.rot >> 1;
   if (r >= rows) return;
@@ -89,7 +73,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeTensor q, RopeTensor k, R
   T* ky = (T*)k.y + (size_t)r * k.y_stride;
   bool ready = false;
   for (int u0 = first; u0 < last; u0 += 64 * U) {
-    u32x4 lo[U], hi[U];
+    P lo[U], hi[U];
     int task[U];
     T* to[U];
 #pragma unroll
@@ -99,12 +83,12 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeTensor q, RopeTensor k, R
       if (u < last) {
         const int h = u / per_head, t = u % per_head;
         const bool is_k = h >= q.heads;
-        const size_t off = (size_t)(is_k ? h - q.heads : h) * d + t * N + (!INTERLEAVED && t >= turning ? half : 0);
+        const size_t off = (size_t)(is_k ? h - q.heads : h) * d + (t < turning ? t * step : a.rot + (t - turning) * N);
         const T* x = (is_k ? kx : qx) + off;
         to[j] = (is_k ? ky : qy) + off;
         task[j] = t;
-        lo[j] = *(const u32x4*)x;
-        if (!INTERLEAVED && t < turning) hi[j] = *(const u32x4*)(x + half);
+        lo[j] = *(const P*)x;
+        if (!INSIDE && t < turning) hi[j] = *(const P*)(x + apart);
       }
     }
     if (!ready) {
@@ -120,49 +104,51 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeTensor q, RopeTensor k, R
       const int t = task[j];
       if (t < 0) continue;
       if (t >= turning) {
-        *(u32x4*)to[j] = lo[j];
-      } else if constexpr (INTERLEAVED) {
+        *(P*)to[j] = lo[j];
+      } else if constexpr (INSIDE) {
         float f[N];
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-          turn(at<T>(lo[j], 2 * i), at<T>(lo[j], 2 * i + 1), cs[wave][t * (N / 2) + i], sn[wave][t * (N / 2) + i], f[2 * i], f[2 * i + 1]);
-        }
-        *(u32x4*)to[j] = piece_of<T>(f);
+        for (int i = 0; i < N / 2; ++i)
+          turn(lo[j].at(2 * i), lo[j].at(2 * i + 1), cs[wave][t * (N / 2) + i], sn[wave][t * (N / 2) + i], f[2 * i], f[2 * i + 1]);
+        lo[j].set(f);
+        *(P*)to[j] = lo[j];
       } else {
         float fa[N], fb[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          turn(at<T>(lo[j], i), at<T>(hi[j], i), cs[wave][t * N + i], sn[wave][t * N + i], fa[i], fb[i]);
-        }
-        *(u32x4*)to[j] = piece_of<T>(fa);
-        *(u32x4*)(to[j] + half) = piece_of<T>(fb);
+        for (int i = 0; i < N; ++i) turn(lo[j].at(i), hi[j].at(i), cs[wave][t * N + i], sn[wave][t * N + i], fa[i], fb[i]);
+        lo[j].set(fa);
+        hi[j].set(fb);
+        *(P*)to[j] = lo[j];
+        *(P*)(to[j] + apart) = hi[j];
       }
     }
   }
 }
 
-bool aligned(const RopeTensor& t, int n, int size) {
+bool aligned(const RopeTensor& t, int size) {
   return !t.x || ((((uintptr_t)t.x | (uintptr_t)t.y) & 15) == 0 && t.stride * size % 16 == 0 && t.y_stride * size % 16 == 0);
 }
 
 template <typename T>
 hipError_t launch(const RopeTensor& q, const RopeTensor& k, const RopeAngles& a, int rows, int d, hipStream_t st) {
-  constexpr int N = Piece<T>::N;
-  const int unit = a.interleaved ? a.rot : a.rot / 2;               // what turning pieces have to fill
-  if (d % N || unit % N || !aligned(q, N, sizeof(T)) || !aligned(k, N, sizeof(T))) {
-    hipLaunchKernelGGL(rope_any_kernel<T>, dim3(rows), dim3(256), 0, st, q, k, a, d);
-    return hipGetLastError();
-  }
-  const int turning = unit / N;
+  constexpr int WIDE = 16 / sizeof(T);
+  const int half = a.rot / 2, unit = a.interleaved ? a.rot : half;                  // what pieces to be rotated have to fill
+  const bool wide = d % WIDE == 0 && unit % WIDE == 0 && aligned(q, sizeof(T)) && aligned(k, sizeof(T));
+  const int n = wide ? WIDE : 1, turning = wide ? unit / WIDE : half;
   const bool in_place = q.x == q.y && (!k.x || k.x == k.y);         // then the rest of a head stays as it is
-  const int per_head = turning + (in_place ? 0 : (d - a.rot) / N), tasks = (q.heads + k.heads) * per_head;
+  const int per_head = turning + (in_place ? 0 : (d - a.rot) / n), tasks = (q.heads + k.heads) * per_head;
   // up to some thousand rows: a row over several wavefronts, each with the row's angles of its own (one / several, us: 4 rows of 72 heads 5.8 / 2.5, of 512 30.0 / 2.6, 1000 rows
   // of 72 9.2 / 6.6, 2047 fp32 rows of 40, half of each head 18.1 / 14.8 out of the last-level cache; an empty launch takes 2.2)
   const int most = (tasks + 63) / 64, want = std::max(1, std::min(most, 8192 / rows));
   const int share = (most + want - 1) / want * 64;
   const dim3 grid((rows + 3) / 4, (tasks + share - 1) / share);
-  if (a.interleaved) hipLaunchKernelGGL((rope_kernel<T, true>), grid, dim3(256), 0, st, q, k, a, rows, d, divisor(per_head), turning, share);
-  else hipLaunchKernelGGL((rope_kernel<T, false>), grid, dim3(256), 0, st, q, k, a, rows, d, divisor(per_head), turning, share);
+  const Divisor by = divisor(per_head);
+  if (!wide)
+    hipLaunchKernelGGL((rope_kernel<T, 1, false>), grid, dim3(256), 0, st, q, k, a, rows, d, by, turning, a.interleaved ? 1 : half, a.interleaved ? 2 : 1, share);
+  else if (a.interleaved)
+    hipLaunchKernelGGL((rope_kernel<T, WIDE, true>), grid, dim3(256), 0, st, q, k, a, rows, d, by, turning, 0, WIDE, share);
+  else
+    hipLaunchKernelGGL((rope_kernel<T, WIDE, false>), grid, dim3(256), 0, st, q, k, a, rows, d, by, turning, half, WIDE, share);
   return hipGetLastError();
 }
 
