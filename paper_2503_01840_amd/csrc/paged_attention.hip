@@ -1,7 +1,7 @@
 // Attention of one new token of every sequence over its paged keys and values (bf16, fp32, or 8 bits with a scale per row):
 // o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m), s_j = scale q.k_j, in one pass with a running maximum m.
 //
-// A wavefront has the (up to 16) query heads of one KV head and walks over tiles of 32 keys (fp32: 16), with a maximum, a sum and an output of its
+// A wavefront has up to 16 or 32 query heads of one KV head and walks over tiles of 32 keys (fp32: 16), with a maximum, a sum and an output of its
 // own; what wavefronts have of one sequence is joined at the end, through LDS within a workgroup, by a second launch between workgroups (paged_rules.hpp says which).
 // Everything a wavefront multiplies comes from global memory straight into the registers where the matrix units want it:
 //   scores  S^T = K Q^T: lane (g, m) = (lane / 16, lane % 16) holds key m of a block of 16, of whose row the four lanes g load 64 contiguous bytes at a time;
@@ -90,20 +90,22 @@ struct Tile {                             // one tile's keys and values, as load
 
 // One (KV head, row tile) of one sequence: queries in registers, the running maximum, sum and output of the tiles that this wavefront has taken.
 // BLOCKED: pages are whole blocks of 16 keys, so that a block's page is looked up once, by scalar loads, and rows lie at fixed distances.
-template <int TYPE, int D, bool BLOCKED>
+// TILES: of 16 query heads each.
+template <int TYPE, int D, bool BLOCKED, int TILES>
 struct Walk {
   typedef Tile<TYPE, D> T;
   typedef typename CacheType<TYPE>::row Row;
   static constexpr bool FP8 = TYPE == PAGED_FP8, F32 = TYPE == PAGED_FP32;
-  static constexpr int BLOCKS = T::BLOCKS, E = T::E, KEYS = 16 * BLOCKS, NF = D / 16;      // NF: products over the values
+  static constexpr int BLOCKS = T::BLOCKS, E = T::E, KEYS = 16 * BLOCKS, NF = D / 16, ROWS = 16 * TILES;      // NF: products over the values
   static constexpr int KB = D * T::SIZE, VB = KB / 16;                                       // bytes of a row, and of a lane's part of a value row
 
   const AttnArgs& p;
   const int lane, m, g;
   int b, n, hk, head0, rows;
-  u32x4 q[FP8 ? 2 * T::KL : T::KL];
-  floatx4 o[NF];
-  float mx, l;                            // of query m; l: over this lane's keys
+  static constexpr int QL = FP8 ? 2 * T::KL : T::KL;
+  u32x4 q[TILES][QL];
+  floatx4 o[TILES][NF];
+  float mx[TILES], l[TILES];              // of queries m, 16 + m; l: over this lane's keys
   const int32_t* table;
   uint32_t row_bytes;
 
@@ -115,21 +117,24 @@ struct Walk {
     b = seq;
     hk = unit % p.by_heads;
     const int rt = unit / p.by_heads;
-    head0 = hk * p.G + rt * PAGED_ROWS;
-    rows = min(PAGED_ROWS, p.G - rt * PAGED_ROWS);
+    head0 = hk * p.G + rt * ROWS;
+    rows = min(ROWS, p.G - rt * ROWS);
     table = p.c.table + (size_t)b * p.c.max_pages;
     // in the order of the keys' dimensions
-    const char* qrow = p.q + (long long)b * p.q_stride + (size_t)(head0 + min(m, rows - 1)) * (D * sizeof(Row));
 #pragma unroll
-    for (int j = 0; j < (int)(sizeof(q) / 16); ++j) {
-      const int at = FP8 ? 64 * (j >> 1) + 16 * g + 8 * (j & 1) : F32 ? 16 * j + 4 * g : 32 * j + 8 * g;
-      q[j] = *(const u32x4*)(qrow + at * sizeof(Row));
-      if (m >= rows) q[j] = u32x4{0, 0, 0, 0};
+    for (int r = 0; r < TILES; ++r) {
+      const char* qrow = p.q + (long long)b * p.q_stride + (size_t)(head0 + min(16 * r + m, rows - 1)) * (D * sizeof(Row));
+#pragma unroll
+      for (int j = 0; j < QL; ++j) {
+        const int at = FP8 ? 64 * (j >> 1) + 16 * g + 8 * (j & 1) : F32 ? 16 * j + 4 * g : 32 * j + 8 * g;
+        q[r][j] = *(const u32x4*)(qrow + at * sizeof(Row));
+        if (16 * r + m >= rows) q[r][j] = u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < NF; ++i) o[r][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+      mx[r] = -FLT_MAX;
+      l[r] = 0.f;
     }
-#pragma unroll
-    for (int i = 0; i < NF; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-    mx = -FLT_MAX;
-    l = 0.f;
   }
 
   // ---- where a tile's rows lie.  BLOCKED: the slots of the first keys of its blocks (uniform); else the slot of one key in every lane.
@@ -207,35 +212,49 @@ struct Walk {
   // ---- products
   template <typename F> __device__ __forceinline__ void work(T& t, int tile, F&& keys_are_used) {
 #pragma clang fp contract(off)            // a score and the maximum that it may be have to be the same number, however large
-    float x[E];                           // scores of keys (g, e), e = 4 block + i
+    float x[TILES][E];                    // scores of keys (g, e), e = 4 block + i
     float kscale[BLOCKS];
     if constexpr (FP8)
 #pragma unroll
       for (int i = 0; i < BLOCKS; ++i) kscale[i] = exp_scale((uint32_t)__builtin_amdgcn_ds_bpermute(from_lane(i), (int)t.exps));
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i) {
-      floatx4 s = {0.f, 0.f, 0.f, 0.f};
-      floatx4 part[4] = {s, s, s, s};     // fp32: four sums of a quarter of the products each, for shorter chains of roundings and of instructions
+      // fp32: four sums of a quarter of the products each, for shorter chains of roundings and of instructions
+      constexpr int SUMS = F32 ? 4 : 1;
+      floatx4 s[TILES][SUMS];
+#pragma unroll
+      for (int r = 0; r < TILES; ++r)
+#pragma unroll
+        for (int h = 0; h < SUMS; ++h) s[r][h] = floatx4{0.f, 0.f, 0.f, 0.f};
+      auto product = [&](const u32x4& a, int j) {
+#pragma unroll
+        for (int r = 0; r < TILES; ++r) s[r][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, q[r][j]), s[r][0], 0, 0, 0);
+      };
 #pragma unroll
       for (int j = 0; j < T::KL; ++j) {
         if constexpr (F32) {
 #pragma unroll
-          for (int h = 0; h < 4; ++h) part[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[i][j][h]), __uint_as_float(q[j][h]), part[h], 0, 0, 0);
+          for (int h = 0; h < 4; ++h)
+#pragma unroll
+            for (int r = 0; r < TILES; ++r)
+              s[r][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[i][j][h]), __uint_as_float(q[r][j][h]), s[r][h], 0, 0, 0);
         } else if constexpr (FP8) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint32_t w0 = t.k[i][j][2 * h], w1 = t.k[i][j][2 * h + 1];
-            const u32x4 a = {bf16_of_codes<false>(w0, kscale[i]), bf16_of_codes<true>(w0, kscale[i]), bf16_of_codes<false>(w1, kscale[i]),
-                             bf16_of_codes<true>(w1, kscale[i])};
-            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, q[2 * j + h]), s, 0, 0, 0);
+            product(u32x4{bf16_of_codes<false>(w0, kscale[i]), bf16_of_codes<true>(w0, kscale[i]), bf16_of_codes<false>(w1, kscale[i]),
+                          bf16_of_codes<true>(w1, kscale[i])}, 2 * j + h);
           }
         } else {
-          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[i][j]), __builtin_bit_cast(bf16x8, q[j]), s, 0, 0, 0);
+          product(t.k[i][j], j);
         }
       }
-      if constexpr (F32) s = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[4 * i + r] = s[r] * p.scale_log2;
+      for (int r = 0; r < TILES; ++r) {
+        if constexpr (F32) s[r][0] = (s[r][0] + s[r][1]) + (s[r][2] + s[r][3]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[r][4 * i + c] = s[r][0][c] * p.scale_log2;
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
     keys_are_used();
@@ -245,77 +264,85 @@ struct Walk {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const bool seen = 16 * (e >> 2) + 4 * g + (e & 3) < left;
-        if (!seen) x[e] = -__builtin_huge_valf();
+#pragma unroll
+        for (int r = 0; r < TILES; ++r)
+          if (!seen) x[r][e] = -__builtin_huge_valf();
 #pragma unroll
         for (int j = 0; j < T::VD; ++j) t.v[e][j] = seen ? t.v[e][j] : 0u;          // a weight of zero does not silence an infinity
       }
       if (16 * (m >> 2 & 1) + 4 * g + (m & 3) >= left) t.exps = 127;                // nor what lies in the place of an exponent
     }
-    float top = x[0];
+    u32x4 head[TILES], tail[TILES];
+    float w[TILES][E];
 #pragma unroll
-    for (int e = 1; e < E; ++e) top = fmaxf(top, x[e]);
-    top = xlane_max_step<5>(xlane_max_step<4>(top));
-    if (__any(top > mx + SLACK)) {
-      const float to = fmaxf(mx, top), a = exp2_fast(mx - to);
-      mx = to;
-      l *= a;
+    for (int r = 0; r < TILES; ++r) {
+      float top = x[r][0];
 #pragma unroll
-      for (int i = 0; i < NF; ++i) o[i] *= a;
+      for (int e = 1; e < E; ++e) top = fmaxf(top, x[r][e]);
+      top = xlane_max_step<5>(xlane_max_step<4>(top));
+      if (__any(top > mx[r] + SLACK)) {
+        const float to = fmaxf(mx[r], top), a = exp2_fast(mx[r] - to);
+        mx[r] = to;
+        l[r] *= a;
+#pragma unroll
+        for (int i = 0; i < NF; ++i) o[r][i] *= a;
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        w[r][e] = exp2_fast(x[r][e] - mx[r]);
+        l[r] += w[r][e];
+      }
+      if constexpr (FP8) static_for<0, E>([&](auto e) { w[r][e] *= exp_scale(bcast16<8 + e>(t.exps)); });
+      // a weight as a head of 8 bits and a tail of 8 more; the tail of a weight above zero is above zero, so that an infinity stays one
+      if constexpr (!F32)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w0 = __float_as_uint(w[r][2 * j]), w1 = __float_as_uint(w[r][2 * j + 1]);
+          head[r][j] = __builtin_amdgcn_perm(w1, w0, 0x07060302u);
+          tail[r][j] = pack_bf16x2(fmaf(__uint_as_float(w0 & 0xFFFF0000u), -0x1.fffffep-1f, w[r][2 * j]),
+                                   fmaf(__uint_as_float(w1 & 0xFFFF0000u), -0x1.fffffep-1f, w[r][2 * j + 1]));
+        }
     }
-    float w[E];
+    auto product = [&](int i, const u32x4& a) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      w[e] = exp2_fast(x[e] - mx);
-      l += w[e];
-    }
+      for (int r = 0; r < TILES; ++r) {
+        o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, head[r]), o[r][i], 0, 0, 0);
+        o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, tail[r]), o[r][i], 0, 0, 0);
+      }
+    };
     if constexpr (F32) {
 #pragma unroll
       for (int e = 0; e < E; ++e)
 #pragma unroll
-        for (int i = 0; i < NF; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[e][i]), w[e], o[i], 0, 0, 0);
-    } else {
-      if constexpr (FP8) {
-        static_for<0, E>([&](auto e) { w[e] *= exp_scale(bcast16<8 + e>(t.exps)); });
-      }
-      // a weight as a head of 8 bits and a tail of 8 more; the tail of a weight above zero is above zero, so that an infinity stays one
-      u32x4 head, tail;
+        for (int i = 0; i < NF; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t w0 = __float_as_uint(w[2 * j]), w1 = __float_as_uint(w[2 * j + 1]);
-        head[j] = __builtin_amdgcn_perm(w1, w0, 0x07060302u);
-        tail[j] = pack_bf16x2(fmaf(__uint_as_float(w0 & 0xFFFF0000u), -0x1.fffffep-1f, w[2 * j]), fmaf(__uint_as_float(w1 & 0xFFFF0000u), -0x1.fffffep-1f, w[2 * j + 1]));
-      }
-      auto product = [&](int i, const u32x4& a) {
-        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, head), o[i], 0, 0, 0);
-        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, tail), o[i], 0, 0, 0);
-      };
-      if constexpr (FP8) {
+          for (int r = 0; r < TILES; ++r) o[r][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[e][i]), w[r][e], o[r][i], 0, 0, 0);
+    } else if constexpr (FP8) {
 #pragma unroll
-        for (int c = 0; c < T::VD; ++c)                      // four dimensions of a dword
+      for (int c = 0; c < T::VD; ++c)                        // four dimensions of a dword
 #pragma unroll
-          for (int hi = 0; hi < 2; ++hi) {
-            u32x4 a0, a1;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t two = __builtin_amdgcn_perm(t.v[2 * j + 1][c], t.v[2 * j][c], hi ? 0x07030602u : 0x05010400u);
-              a0[j] = bf16_of_codes<false>(two, 1.f);
-              a1[j] = bf16_of_codes<true>(two, 1.f);
-            }
-            product(4 * c + 2 * hi, a0);
-            product(4 * c + 2 * hi + 1, a1);
-          }
-      } else {
-#pragma unroll
-        for (int c = 0; c < T::VD; ++c) {
+        for (int hi = 0; hi < 2; ++hi) {
           u32x4 a0, a1;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            a0[j] = __builtin_amdgcn_perm(t.v[2 * j + 1][c], t.v[2 * j][c], 0x05040100u);
-            a1[j] = __builtin_amdgcn_perm(t.v[2 * j + 1][c], t.v[2 * j][c], 0x07060302u);
+            const uint32_t two = __builtin_amdgcn_perm(t.v[2 * j + 1][c], t.v[2 * j][c], hi ? 0x07030602u : 0x05010400u);
+            a0[j] = bf16_of_codes<false>(two, 1.f);
+            a1[j] = bf16_of_codes<true>(two, 1.f);
           }
-          product(2 * c, a0);
-          product(2 * c + 1, a1);
+          product(4 * c + 2 * hi, a0);
+          product(4 * c + 2 * hi + 1, a1);
         }
+    } else {
+#pragma unroll
+      for (int c = 0; c < T::VD; ++c) {
+        u32x4 a0, a1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          a0[j] = __builtin_amdgcn_perm(t.v[2 * j + 1][c], t.v[2 * j][c], 0x05040100u);
+          a1[j] = __builtin_amdgcn_perm(t.v[2 * j + 1][c], t.v[2 * j][c], 0x07060302u);
+        }
+        product(2 * c, a0);
+        product(2 * c + 1, a1);
       }
     }
   }
@@ -347,15 +374,19 @@ struct Walk {
       t.exps = exps;
     }
     work(t, i, [] {});
-    l = xlane_sum_step<5>(xlane_sum_step<4>(l));
+#pragma unroll
+    for (int r = 0; r < TILES; ++r) l[r] = xlane_sum_step<5>(xlane_sum_step<4>(l[r]));
   }
 
-  // dimension NF * (4 g + r) + i of query m
+  // f(query, tile, first of four dimensions, their sums): of query m of a tile this lane has the dimensions NF * (4 g + c) + i
   template <typename F> __device__ __forceinline__ void each4(F&& f) const {
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < TILES; ++r)
+      if (16 * r + m < rows)
 #pragma unroll
-      for (int i = 0; i < NF; i += 4) f(NF * (4 * g + r) + i, floatx4{o[i][r], o[i + 1][r], o[i + 2][r], o[i + 3][r]});
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < NF; i += 4) f(16 * r + m, r, NF * (4 * g + c) + i, floatx4{o[r][i][c], o[r][i + 1][c], o[r][i + 2][c], o[r][i + 3][c]});
   }
 };
 
@@ -369,11 +400,12 @@ __device__ __forceinline__ int length_of(const AttnArgs& p, int b) { return min(
 // The results of a workgroup's wavefronts, joined: f(row, first of four dimensions, their sums, maximum, sum of weights).
 template <typename W, int D, typename F>
 __device__ __forceinline__ void join_team(const W& w, int wave, int active, F&& f) {
-  __shared__ __attribute__((aligned(16))) float so[WAVES][PAGED_ROWS][D + 4], sml[WAVES][PAGED_ROWS][2];
-  if (w.m < w.rows && wave < active) {
-    if (w.g == 0) { sml[wave][w.m][0] = w.mx; sml[wave][w.m][1] = w.l; }
-    w.each4([&](int d, const floatx4& v) { *(floatx4*)&so[wave][w.m][d] = v; });
-  }
+  __shared__ __attribute__((aligned(16))) float so[WAVES][W::ROWS][D + 4], sml[WAVES][W::ROWS][2];
+  if (wave < active)
+    w.each4([&](int row, int r, int d, const floatx4& v) {
+      *(floatx4*)&so[wave][row][d] = v;
+      if (d == 0) { sml[wave][row][0] = w.mx[r]; sml[wave][row][1] = w.l[r]; }
+    });
   __syncthreads();
   for (int u = threadIdx.x; u < w.rows * (D / 4); u += 64 * WAVES) {
     const int row = u / (D / 4), d = u % (D / 4) * 4;
@@ -431,9 +463,9 @@ __device__ __forceinline__ int longest_first(const AttnArgs& p, int wave, int at
 
 // Short contexts, or very many: a workgroup per sequence and unit; one launch.  Where there are more workgroups than CUs, those of long sequences
 // begin first: 64 of 512..2048 tokens, 32 heads over 8, bf16 76.6 -> 65.2 us.
-template <int TYPE, int D, bool BLOCKED>
+template <int TYPE, int D, bool BLOCKED, int TILES>
 __global__ __launch_bounds__(64 * WAVES) void paged_whole_kernel(AttnArgs p) {
-  typedef Walk<TYPE, D, BLOCKED> W;
+  typedef Walk<TYPE, D, BLOCKED, TILES> W;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = p.B > 1 && (long long)p.B * p.units > 256 ? longest_first(p, wave, blockIdx.y) : (int)blockIdx.y;
   W w(p);
   w.begin(b, blockIdx.x);
@@ -462,9 +494,9 @@ template <int KEYS> __device__ __forceinline__ int scan_tiles(const AttnArgs& p,
 // Longer contexts: all sequences' tiles in equal ranges; the parts of sequences that do not lie within one range are joined by the next kernel.
 // TEAM: a workgroup has a range of one unit.  Else a wavefront has, and the wavefronts of a workgroup have the units of one range after the other, so that together
 // they read whole rows.
-template <int TYPE, int D, bool BLOCKED, bool TEAM>
+template <int TYPE, int D, bool BLOCKED, int TILES, bool TEAM>
 __global__ __launch_bounds__(64 * WAVES) void paged_ranges_kernel(AttnArgs p) {
-  typedef Walk<TYPE, D, BLOCKED> W;
+  typedef Walk<TYPE, D, BLOCKED, TILES> W;
   constexpr int STEP = TEAM ? WAVES : 1;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = TEAM ? blockIdx.x : (int)blockIdx.x * WAVES + wave;
   const int range = at / p.by_units, unit = at % p.by_units, offset = TEAM ? wave : 0;
@@ -492,10 +524,10 @@ __global__ __launch_bounds__(64 * WAVES) void paged_ranges_kernel(AttnArgs p) {
         else store_part<D>(p, range, b, w.head0 + row, d, sum, M, L);
       });
       if (stop < last) __syncthreads();
-    } else if (w.m < w.rows) {
-      const int h = w.head0 + w.m;
-      if (whole) w.each4([&](int d, const floatx4& v) { store_result<W::F32, D>(p, b, h, d, v, w.mx, w.l); });
-      else w.each4([&](int d, const floatx4& v) { store_part<D>(p, range, b, h, d, v, w.mx, w.l); });
+    } else if (whole) {
+      w.each4([&](int row, int r, int d, const floatx4& v) { store_result<W::F32, D>(p, b, w.head0 + row, d, v, w.mx[r], w.l[r]); });
+    } else {
+      w.each4([&](int row, int r, int d, const floatx4& v) { store_part<D>(p, range, b, w.head0 + row, d, v, w.mx[r], w.l[r]); });
     }
     x = stop;
   }
@@ -567,15 +599,15 @@ __global__ __launch_bounds__(512) void paged_join_kernel(AttnArgs p) {
   if (lane < DL && h < p.H) store_result<F32, D>(p, b, h, d, j.sum, j.M, j.L);
 }
 
-template <int TYPE, int D, bool BLOCKED>
+template <int TYPE, int D, bool BLOCKED, int TILES>
 hipError_t launch(const AttnArgs& a, const PagedSplit& s, hipStream_t st) {
   if (s.ranges == 0) {
-    hipLaunchKernelGGL((paged_whole_kernel<TYPE, D, BLOCKED>), dim3(a.units, a.B), dim3(64 * WAVES), 0, st, a);
+    hipLaunchKernelGGL((paged_whole_kernel<TYPE, D, BLOCKED, TILES>), dim3(a.units, a.B), dim3(64 * WAVES), 0, st, a);
     return hipGetLastError();
   }
   const int n = s.ranges * a.units;
-  if (s.team) hipLaunchKernelGGL((paged_ranges_kernel<TYPE, D, BLOCKED, true>), dim3(n), dim3(64 * WAVES), 0, st, a);
-  else hipLaunchKernelGGL((paged_ranges_kernel<TYPE, D, BLOCKED, false>), dim3((n + WAVES - 1) / WAVES), dim3(64 * WAVES), 0, st, a);
+  if (s.team) hipLaunchKernelGGL((paged_ranges_kernel<TYPE, D, BLOCKED, TILES, true>), dim3(n), dim3(64 * WAVES), 0, st, a);
+  else hipLaunchKernelGGL((paged_ranges_kernel<TYPE, D, BLOCKED, TILES, false>), dim3((n + WAVES - 1) / WAVES), dim3(64 * WAVES), 0, st, a);
   constexpr int KEYS = 16 * CacheType<TYPE>::BLOCKS;
   constexpr bool F32 = TYPE == PAGED_FP32;
   if (s.ranges / a.B > 16) hipLaunchKernelGGL((paged_join_kernel<KEYS, F32, D, 8, 8>), dim3(a.H, a.B, D / 32), dim3(512), 0, st, a);
@@ -586,23 +618,26 @@ hipError_t launch(const AttnArgs& a, const PagedSplit& s, hipStream_t st) {
 // 1000..2048) 42.7 against 45.5.
 template <int TYPE, int D>
 hipError_t launch(const AttnArgs& a, const PagedSplit& s, hipStream_t st) {
-  return a.c.page.d % 16 == 0 ? launch<TYPE, D, true>(a, s, st) : launch<TYPE, D, false>(a, s, st);
+  if constexpr (TYPE != PAGED_FP32)
+    if (s.rows == 32) return a.c.page.d % 16 == 0 ? launch<TYPE, D, true, 2>(a, s, st) : launch<TYPE, D, false, 2>(a, s, st);
+  return a.c.page.d % 16 == 0 ? launch<TYPE, D, true, 1>(a, s, st) : launch<TYPE, D, false, 1>(a, s, st);
+}
+
+PagedSplit split_of(const PagedView& c, int dtype, int B, int H, int max_len) {
+  return paged_split(B, H, c.Hkv, c.d * (dtype == PAGED_FP32 ? 4 : dtype == PAGED_BF16 ? 2 : 1), dtype == PAGED_FP32, max_len);
 }
 
 }  // namespace
 
-static int cached_row_bytes(const PagedView& c, int dtype) { return c.d * (dtype == PAGED_FP32 ? 4 : dtype == PAGED_BF16 ? 2 : 1); }
-
 size_t paged_attention_workspace(const PagedView& c, int dtype, int B, int H, int max_len) {
-  return paged_partial_floats(B, H, c.d, paged_split(B, H, c.Hkv, cached_row_bytes(c, dtype), max_len).ranges) * sizeof(float);
+  return paged_partial_floats(B, H, c.d, split_of(c, dtype, B, H, max_len).ranges) * sizeof(float);
 }
 
 hipError_t launch_paged_attention(const PagedView& c, int dtype, int B, int H, const void* q, long long q_bytes, const int32_t* kv_len, int max_len,
                                   float scale, void* out, float* lse, void* workspace, hipStream_t st) {
-  const int units = paged_units(H, c.Hkv);
-  const PagedSplit s = paged_split(B, H, c.Hkv, cached_row_bytes(c, dtype), max_len);
+  const PagedSplit s = split_of(c, dtype, B, H, max_len);
   float* part_o = (float*)workspace;
-  const AttnArgs a = {c, (const char*)q, q_bytes, kv_len, max_len, H, H / c.Hkv, B, units, s.ranges, divisor(units), divisor(c.Hkv),
+  const AttnArgs a = {c, (const char*)q, q_bytes, kv_len, max_len, H, H / c.Hkv, B, s.units, s.ranges, divisor(s.units), divisor(c.Hkv),
                       scale * 1.4426950408889634f, out, lse, part_o, part_o ? part_o + (size_t)(s.ranges + B) * H * c.d : nullptr};
   if (dtype == PAGED_FP8) return c.d == 128 ? launch<PAGED_FP8, 128>(a, s, st) : launch<PAGED_FP8, 64>(a, s, st);
   if (dtype == PAGED_BF16) return c.d == 128 ? launch<PAGED_BF16, 128>(a, s, st) : launch<PAGED_BF16, 64>(a, s, st);

@@ -122,6 +122,14 @@ def test_bounds_ahead_of_the_lengths(dtype, B, bound):
     _check(c, wide, q, [0 if n % 3 == 0 else n for n in lens], out, lse)
 
 
+# more than 16 query heads to a KV head: two products of each operand, in parts and whole, in pages of either kind; a last tile of 1, 8, 16 heads
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("H,Hkv,d,page,lens", [(24, 1, 128, 16, [40000, 0, 30001]), (17, 1, 64, 20, [70001]), (64, 2, 64, 48, [20000, 17000]), (33, 1, 128, 24, [66000]),
+                                               (96, 4, 64, 16, [700, 0, 33] * 28), (32, 1, 128, 7, [700, 16, 31] * 33)])
+def test_many_query_heads_to_a_kv_head(dtype, H, Hkv, d, page, lens):
+    _run(dtype, H, Hkv, d, page, lens, H)
+
+
 # enough keys for a range to every wavefront, in pages of whole blocks of 16 keys and in others
 @pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
 @pytest.mark.parametrize("page", [48, 20])

@@ -40,16 +40,19 @@ int main() {
     for (int Hkv : {1, 2, 8, 40, 300, 65535})
       for (int G : {1, 4, 16, 17, 64})
         for (int n : {1, 511, 512, 513, 1024, 1025, 4096, 131072, 1 << 30}) {
-          const int H = Hkv * G, units = paged_units(H, Hkv), total = 0;
-          const PagedSplit s = paged_split(B, H, Hkv, 128 << (B & 1), n);
-          const int ranges = s.ranges;
-          NEED(units == Hkv * ((G + 15) / 16));
+          const int H = Hkv * G, total = 0;
+          const bool fp32 = B & 1;
+          const PagedSplit s = paged_split(B, H, Hkv, 128 << (B & 1), fp32, n);
+          const int ranges = s.ranges, units = s.units;
+          NEED((s.rows == 16 || (s.rows == 32 && !fp32 && G > 16)) && units == Hkv * ((G + s.rows - 1) / s.rows));
           NEED(ranges >= 0 && ranges <= 256 * PAGED_WAVES);
           NEED(ranges == 0 || ((long)B * (n / 16 + 1) < 1l << 30 && B <= 1024 && (long)ranges * units <= std::max(256l * PAGED_WAVES, (long)units)));
           NEED(n > 768 || ranges == 0);
+          NEED(s.team || ranges == 0 || units >= 8);
         }
-  const PagedSplit a = paged_split(1, 32, 8, 256, 4096), b = paged_split(1, 64, 8, 128, 131072), c = paged_split(64, 32, 8, 128, 2048), d = paged_split(64, 32, 8, 256, 2048);
-  printf("%d %d  %d %d  %d %d  %d\\n", a.ranges, a.team, b.ranges, b.team, c.ranges, c.team, d.ranges);
+  const PagedSplit a = paged_split(1, 32, 8, 256, false, 4096), b = paged_split(1, 64, 8, 128, false, 131072), c = paged_split(64, 32, 8, 128, false, 2048),
+                   d = paged_split(64, 32, 8, 256, false, 2048), e = paged_split(19, 24, 1, 128, false, 103066), f = paged_split(4, 24, 1, 256, false, 700);
+  printf("%d %d  %d %d  %d %d  %d  %d %d %d  %d %d\\n", a.ranges, a.team, b.ranges, b.team, c.ranges, c.team, d.ranges, e.rows, e.ranges, e.team, f.rows, f.units);
   return 0;
 }
 '''
@@ -61,4 +64,4 @@ def test_division_of_tiles_and_the_rule(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O2", "-I", inc, str(tmp_path / "m.cpp"), "-o", str(tmp_path / "m")], check=True)
     r = subprocess.run([str(tmp_path / "m")], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
-    assert r.stdout.split() == ["32", "1", "256", "0", "256", "0", "0"]
+    assert r.stdout.split() == "32 1 256 0 256 0 0 32 256 1 16 2".split()
