@@ -29,6 +29,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int WAVES = PAGED_WAVES;
 constexpr float SLACK = 8.f;              // the running maximum moves when a score exceeds it by more than 2^8
 
+// What a kernel needs for its first loads comes in arguments of its own as well, which are in registers when it starts (one sequence of 4096 tokens 10.2 -> 9.8 us, of 128
+// 4.55 -> 4.46).
 struct AttnArgs {
   PagedView c;
   const char* q;
@@ -464,7 +466,9 @@ __device__ __forceinline__ int longest_first(const AttnArgs& p, int wave, int at
 // Short contexts, or very many: a workgroup per sequence and unit; one launch.  Where there are more workgroups than CUs, those of long sequences
 // begin first: 64 of 512..2048 tokens, 32 heads over 8, bf16 76.6 -> 65.2 us.
 template <int TYPE, int D, bool BLOCKED, int TILES>
-__global__ __launch_bounds__(64 * WAVES) void paged_whole_kernel(AttnArgs p) {
+__global__ __launch_bounds__(64 * WAVES) void paged_whole_kernel(const int32_t* kv_len, const int32_t* table, int B, int max_len, int max_pages, int tokens, Divisor page,
+                                                             int n_pages, AttnArgs p) {
+  p.kv_len = kv_len, p.B = B, p.max_len = max_len, p.c.table = table, p.c.max_pages = max_pages, p.c.tokens = tokens, p.c.page = page, p.c.n_pages = n_pages;
   typedef Walk<TYPE, D, BLOCKED, TILES> W;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = p.B > 1 && (long long)p.B * p.units > 256 ? longest_first(p, wave, blockIdx.y) : (int)blockIdx.y;
   W w(p);
@@ -495,7 +499,8 @@ template <int KEYS> __device__ __forceinline__ int scan_tiles(const AttnArgs& p,
 // TEAM: a workgroup has a range of one unit.  Else a wavefront has, and the wavefronts of a workgroup have the units of one range after the other, so that together
 // they read whole rows.
 template <int TYPE, int D, bool BLOCKED, int TILES, bool TEAM>
-__global__ __launch_bounds__(64 * WAVES) void paged_ranges_kernel(AttnArgs p) {
+__global__ __launch_bounds__(64 * WAVES) void paged_ranges_kernel(const int32_t* kv_len, int B, int max_len, int ranges, Divisor by_units, AttnArgs p) {
+  p.kv_len = kv_len, p.B = B, p.max_len = max_len, p.ranges = ranges, p.by_units = by_units;
   typedef Walk<TYPE, D, BLOCKED, TILES> W;
   constexpr int STEP = TEAM ? WAVES : 1;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = TEAM ? blockIdx.x : (int)blockIdx.x * WAVES + wave;
@@ -549,7 +554,8 @@ struct Joint {
 // parts at a time as they have such groups, four of them in flight; groups are joined by exchanges within a wavefront, then through LDS.
 // Few parts: a wavefront to a head with all its dimensions.  Many (131072 tokens under 64 heads: 256 parts): eight, with 32 dimensions, 8.1 -> 5.8 us.
 template <int KEYS, bool F32, int D, int DL, int WAVES_PER>
-__global__ __launch_bounds__(512) void paged_join_kernel(AttnArgs p) {
+__global__ __launch_bounds__(512) void paged_join_kernel(const int32_t* kv_len, int B, int max_len, int ranges, int H, float* part_ml, float* part_o, AttnArgs p) {
+  p.kv_len = kv_len, p.B = B, p.max_len = max_len, p.ranges = ranges, p.H = H, p.part_ml = part_ml, p.part_o = part_o;
   constexpr int PER = 64 * WAVES_PER / DL, HEADS = 8 / WAVES_PER;
   __shared__ __attribute__((aligned(16))) float so[8][4 * DL], sml[8][2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.x * HEADS + wave / WAVES_PER, b = blockIdx.y, n = length_of(p, b);
@@ -601,17 +607,21 @@ __global__ __launch_bounds__(512) void paged_join_kernel(AttnArgs p) {
 
 template <int TYPE, int D, bool BLOCKED, int TILES>
 hipError_t launch(const AttnArgs& a, const PagedSplit& s, hipStream_t st) {
-  if (s.ranges == 0) {
-    hipLaunchKernelGGL((paged_whole_kernel<TYPE, D, BLOCKED, TILES>), dim3(a.units, a.B), dim3(64 * WAVES), 0, st, a);
-    return hipGetLastError();
-  }
-  const int n = s.ranges * a.units;
-  if (s.team) hipLaunchKernelGGL((paged_ranges_kernel<TYPE, D, BLOCKED, TILES, true>), dim3(n), dim3(64 * WAVES), 0, st, a);
-  else hipLaunchKernelGGL((paged_ranges_kernel<TYPE, D, BLOCKED, TILES, false>), dim3((n + WAVES - 1) / WAVES), dim3(64 * WAVES), 0, st, a);
   constexpr int KEYS = 16 * CacheType<TYPE>::BLOCKS;
   constexpr bool F32 = TYPE == PAGED_FP32;
-  if (s.ranges / a.B > 16) hipLaunchKernelGGL((paged_join_kernel<KEYS, F32, D, 8, 8>), dim3(a.H, a.B, D / 32), dim3(512), 0, st, a);
-  else hipLaunchKernelGGL((paged_join_kernel<KEYS, F32, D, D / 4, 1>), dim3((a.H + 7) / 8, a.B), dim3(512), 0, st, a);
+  const dim3 team(64 * WAVES);
+  if (s.ranges == 0) {
+    hipLaunchKernelGGL((paged_whole_kernel<TYPE, D, BLOCKED, TILES>), dim3(a.units, a.B), team, 0, st, a.kv_len, a.c.table, a.B, a.max_len, a.c.max_pages, a.c.tokens,
+                       a.c.page, a.c.n_pages, a);
+    return hipGetLastError();
+  }
+  auto ranges = [&](auto kernel, int workgroups) { hipLaunchKernelGGL(kernel, dim3(workgroups), team, 0, st, a.kv_len, a.B, a.max_len, a.ranges, a.by_units, a); };
+  auto join = [&](auto kernel, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(512), 0, st, a.kv_len, a.B, a.max_len, a.ranges, a.H, a.part_ml, a.part_o, a); };
+  const int n = s.ranges * a.units;
+  if (s.team) ranges(paged_ranges_kernel<TYPE, D, BLOCKED, TILES, true>, n);
+  else ranges(paged_ranges_kernel<TYPE, D, BLOCKED, TILES, false>, (n + WAVES - 1) / WAVES);
+  if (s.ranges / a.B > 16) join(paged_join_kernel<KEYS, F32, D, 8, 8>, dim3(a.H, a.B, D / 32));
+  else join(paged_join_kernel<KEYS, F32, D, D / 4, 1>, dim3((a.H + 7) / 8, a.B));
   return hipGetLastError();
 }
 // Pages of whole blocks of 16 keys against any others, the sizes above: 64.7 against 67.1 us (pages of 16, of 100 tokens), 8 bits 42.9 against 43.7, fp32 (16 sequences of
