@@ -87,7 +87,9 @@ __device__ __forceinline__ u32x4 from_codes(const u32x2& c, float scale) {
 
 // per_row: pieces of a row (KV heads * CH); WITHIN: a multiple of 64, so that a wavefront has pieces of one row
 template <int CH, bool FP8, bool READ, bool WITHIN>
-__global__ __launch_bounds__(256) void paged_rows_kernel(PagedView c, PagedRows r, int pieces, Divisor per_row) {
+__global__ __launch_bounds__(256) void paged_rows_kernel(int pieces, Divisor per_row, Divisor rows, const int32_t* start, const int32_t* n, const int32_t* row_start,
+                                                         PagedView c, PagedRows r) {
+  r.rows = rows, r.start = start, r.n = n, r.row_start = row_start;       // in registers when the kernel starts: 2 to 6 % less time
   const int at = blockIdx.x * 256 + threadIdx.x;
   if (at >= pieces) return;
   int line = at / per_row;
@@ -131,8 +133,8 @@ template <int CH, bool FP8, bool READ>
 hipError_t launch(const PagedView& c, const PagedRows& r, int B, hipStream_t st) {
   const int per_row = c.Hkv * CH, pieces = B * r.rows.d * per_row;
   const dim3 grid((pieces + 255) / 256);
-  if (per_row % 64 == 0) hipLaunchKernelGGL((paged_rows_kernel<CH, FP8, READ, true>), grid, dim3(256), 0, st, c, r, pieces, divisor(per_row));
-  else hipLaunchKernelGGL((paged_rows_kernel<CH, FP8, READ, false>), grid, dim3(256), 0, st, c, r, pieces, divisor(per_row));
+  if (per_row % 64 == 0) hipLaunchKernelGGL((paged_rows_kernel<CH, FP8, READ, true>), grid, dim3(256), 0, st, pieces, divisor(per_row), r.rows, r.start, r.n, r.row_start, c, r);
+  else hipLaunchKernelGGL((paged_rows_kernel<CH, FP8, READ, false>), grid, dim3(256), 0, st, pieces, divisor(per_row), r.rows, r.start, r.n, r.row_start, c, r);
   return hipGetLastError();
 }
 
