@@ -3,7 +3,7 @@
 // A thread has 16 bytes of a dense key row and the same of the value row; CH = head_dim * element size / 16 neighbouring lanes have a head, whose
 // largest magnitude they find by exchanges within 16 lanes.  A power of two as the scale makes the scaling and the way back exact: a
 // value is rounded once, to a code.  Where a wavefront lies within one row (a row of 64 pieces and more), its place is looked up with
-// scalar loads.  Bound by bytes; a thread has 32 of them in flight and nothing else waits, so eight wavefronts a SIMD cover the latency: 20480 rows of 8 heads of 128 read
+// scalar loads (40954 rows of 8 heads into 8 bits 54 us, by every lane for itself 68).  Bound by bytes; a thread has 32 of them in flight and nothing else waits, so eight wavefronts a SIMD cover the latency: 20480 rows of 8 heads of 128 read
 // back from 8 bits in 26.5 us (4.8 TB/s, a large copy's rate; 106 by a wavefront to a head and two bytes to a lane), 8960 written in 12.6 (4.4 TB/s; 45).
 #include "paged.hpp"
 

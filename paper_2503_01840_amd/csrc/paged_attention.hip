@@ -13,8 +13,8 @@
 // tile ahead of the products.  8-bit rows become bf16 by an exact conversion (a value row's scale multiplies its weight instead: a conversion takes two keys).
 //
 // Bound by bytes: 64 sequences of 512..2048 tokens, 32 heads of 128 over 8, bf16: 64.0 us, 5.2 TB/s (8 bits: 40.0 us, of which 4.8 join); one of 131071
-// under 64 heads in 8 bits 56.9 us, 5.2 TB/s and 5.6 us of joining; 256 of 1300 in bf16 237 us, 5.7 TB/s.  A tile is 16 (score) or 16 to 32 (value) products and some
-// 250 vector instructions, a fifth of the time that its bytes take.  Two tiles of registers in flight in turn took 211 registers and 4 % longer than
+// under 64 heads in 8 bits 56.9 us, 5.2 TB/s and 5.6 us of joining; 256 of 1300 in bf16 237 us, 5.7 TB/s.  A tile of 128 dimensions is 8 score and 16 value products and some
+// 180 (bf16) or 230 (8 bits) vector instructions, 10 and 20 % of the time that its bytes take.  Two tiles of registers in flight in turn took 211 registers and 4 % longer than
 // one whose halves are asked for again as soon as they are used (150).
 #include <cfloat>
 
