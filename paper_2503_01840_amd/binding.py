@@ -521,6 +521,7 @@ class PagedKVCache:
         self.row_dtype, self.gpu = torch.bfloat16 if fp8 else k.dtype, gpu
         n_pages, page_size, self.heads, self.d = k.shape
         self.B, max_pages = page_table.shape
+        self.sizes = (k.dtype, self.heads, self.d, max_pages * page_size)
         exps = [_arg(x, torch.uint8, k.shape[:3], gpu, "scale exponents") if fp8 else None for x in (k_exp, v_exp)]
         self.c = PagedKV(_arg(k, k.dtype, k.shape, gpu, "k"), _arg(v, k.dtype, k.shape, gpu, "v"), *exps,
                          _arg(page_table, torch.int32, page_table.shape, gpu, "page_table"), _POOL_TYPES[k.dtype], n_pages, page_size, max_pages,
@@ -531,9 +532,9 @@ def _paged_rows(call, cache, k, v, start, n, rows, row_start):
     gpu, B, i32 = cache.gpu, cache.B, torch.int32
     kp, stride = _rows_arg(k, cache.row_dtype, None, cache.heads, cache.d, gpu, "k rows")
     n_rows = k.shape[0]
-    vp, v_stride = _rows_arg(v, cache.row_dtype, n_rows, cache.heads, cache.d, gpu, "v rows")
-    if stride != v_stride:
-        _refuse("v rows", "the row stride of the k rows", v)
+    if v.dtype is not k.dtype or v.get_device() != gpu or v.shape != k.shape or (v.stride() != k.stride() and n_rows > 1):
+        _refuse("v rows", f"what the k rows are ({k.dtype} {tuple(k.shape)}, strides {k.stride()}, on {k.device})", v)
+    vp = v.data_ptr()
     if rows is None:
         rows = n_rows // B
         if row_start is not None:
@@ -561,6 +562,21 @@ def eagle3_paged_read(cache, start=None, n=None, rows=None, row_start=None, out=
     return tuple(out)
 
 
+_workspaces = {}                                              # bytes by sizes: the layers of a step ask for the same
+
+
+def _attention_workspace(cache, B, H, max_kv_len):
+    key = (cache.sizes, B, H, max_kv_len)
+    need = _workspaces.get(key)
+    if need is None:
+        n = C.c_size_t()
+        _check(lib().eagle3_paged_attention_workspace(cache.c, B, H, max_kv_len, n))
+        if len(_workspaces) >= 256:
+            _workspaces.clear()
+        need = _workspaces[key] = n.value
+    return need
+
+
 def eagle3_paged_attention(cache, q, kv_len, max_kv_len, scale=None, out=None, want_lse=False):
     """q [B, H, d] over each sequence's first kv_len[b] <= max_kv_len tokens; scale: 1 / sqrt(d) by default.  Returns out [B, H, d], with
     want_lse also the log of the softmax's sum, fp32 [B, H]."""
@@ -572,11 +588,9 @@ def eagle3_paged_attention(cache, q, kv_len, max_kv_len, scale=None, out=None, w
         to = out.data_ptr()
     else:
         to = _arg(out, dtype, (B, H, d), gpu, "out")
-    lse = torch.empty((B, H), dtype=torch.float32, device=q.device) if want_lse else None
-    need = C.c_size_t()
-    _check(L.eagle3_paged_attention_workspace(cache.c, B, H, max_kv_len, need))
-    need = need.value
-    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    lse = q.new_empty((B, H), dtype=torch.float32) if want_lse else None
+    need = _attention_workspace(cache, B, H, max_kv_len)
+    ws = q.new_empty(need, dtype=torch.uint8) if need else None
     _on(gpu, L.eagle3_paged_attention, cache.c, B, H, qp, stride, _arg(kv_len, torch.int32, (B,), gpu, "kv_len"), max_kv_len,
         d ** -0.5 if scale is None else scale, to, None if lse is None else lse.data_ptr(),
         None if ws is None else ws.data_ptr(), need)
