@@ -394,7 +394,7 @@ def eagle3_ttt_attention(q, k_steps, v_steps):
 
 # ---- rotary positions and a cache in pages: calls without a context
 # These are called once and more a layer and decoding step, with little for the GPU to do in each: what follows looks at every argument, but puts
-# messages together only for those that are refused (25 -> 9 us a call of eagle3_rope, of which 5 are the launch).
+# messages together only for those that are refused (a call of eagle3_rope 25 -> 9 us, of which 3.5 are the launch).
 def _refuse(what, wanted, t):
     raise ValueError(f"{what}: {wanted} is wanted, got " + (f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}" if isinstance(t, torch.Tensor) else repr(t)))
 
@@ -406,16 +406,14 @@ def _arg(t, dtype, shape, gpu, what):
     return t.data_ptr()
 
 
-def _rows_arg(t, dtype, rows, heads, d, gpu, what):
-    """The address and row stride of [rows, heads, d] rows, each dense, any distance apart; heads None: any number."""
-    ok = t.dtype is dtype and t.get_device() == gpu and t.dim() == 3
-    if ok:
-        n, h, m = t.shape
+def _rows_of(t, dtype, gpu, what):
+    """(address, rows, heads, d, row stride) of [rows, heads, d] rows, each with its heads one behind the other, any distance apart."""
+    if t.dtype is dtype and t.get_device() == gpu and t.dim() == 3:
+        n, h, d = t.shape
         s0, s1, s2 = t.stride()
-        ok = (rows is None or n == rows) and (heads is None or h == heads) and m == d and s2 == 1 and (s1 == d or h == 1) and (s0 >= h * d or n <= 1)
-    if not ok:
-        _refuse(what, f"{dtype} rows [{rows}, {heads}, {d}], each with its heads one behind the other, on cuda:{gpu}", t)
-    return t.data_ptr(), s0 if n > 1 else h * d
+        if s2 == 1 and (s1 == d or h == 1) and (s0 >= h * d or n <= 1):
+            return t.data_ptr(), n, h, d, s0 if n > 1 else h * d
+    _refuse(what, f"{dtype} rows [rows, heads, d], each with its heads one behind the other, on cuda:{gpu}", t)
 
 
 def _gpu_of(t, what):
@@ -461,32 +459,37 @@ class Rope:
 _ROPE_TYPES = {torch.bfloat16: EAGLE3_BF16, torch.float32: EAGLE3_FP32}
 
 
-def _rotated(x, y, dtype, rows, heads, d, gpu, what):
-    """Addresses and row strides of x and of where it goes: y, or a new dense tensor, which is returned too."""
-    p, stride = _rows_arg(x, dtype, rows, heads, d, gpu, what)
-    if y is None:
-        y = torch.empty_like(x, memory_format=torch.contiguous_format)
-        return p, stride, y.data_ptr(), x.shape[1] * d, y
-    to, y_stride = _rows_arg(y, dtype, rows, x.shape[1], d, gpu, "out of " + what)
-    return p, stride, to, y_stride, y
+def _place(out, x, rows, heads, d, gpu, what):
+    """Where x's rotated rows go, its address and row stride: `out`, or a new dense tensor."""
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        return out, out.data_ptr(), heads * d
+    p, n, h, m, stride = _rows_of(out, x.dtype, gpu, what)
+    if n != rows or h != heads or m != d:
+        _refuse(what, f"[{rows}, {heads}, {d}]", out)
+    return out, p, stride
 
 
 def _rotate(call, rope, positions, q, k, out):
-    gpu, dtype = _gpu_of(q, "q"), q.dtype
+    gpu, dtype = q.get_device(), q.dtype
     code = _ROPE_TYPES.get(dtype)
-    if code is None or q.dim() != 3 or rope.gpu != gpu:
-        _refuse("q", f"bf16 or fp32 [rows, heads, d] on cuda:{rope.gpu}", q)
-    rows, H, d = q.shape
+    if code is None or gpu < 0 or rope.gpu != gpu:
+        _refuse("q", "a bf16 or fp32 tensor on the GPU of the table of angles", q)
+    qp, rows, H, d, q_stride = _rows_of(q, dtype, gpu, "q")
     pos = _arg(positions, torch.int32, (rows,), gpu, "positions")
     q_out, k_out = out if isinstance(out, (tuple, list)) else (out, None)
-    qp, q_stride, qo, qo_stride, q_out = _rotated(q, q_out, dtype, rows, H, d, gpu, "q")
     if k is None:
         if k_out is not None:
             _refuse("out of k", "None without k", k_out)
+        q_out, qo, qo_stride = _place(q_out, q, rows, H, d, gpu, "out of q")
         _on(gpu, call, code, rows, d, rope.c, pos, H, qp, q_stride, qo, qo_stride, 0, None, 0, None, 0)
         return q_out
-    kp, k_stride, ko, ko_stride, k_out = _rotated(k, k_out, dtype, rows, None, d, gpu, "k")
-    _on(gpu, call, code, rows, d, rope.c, pos, H, qp, q_stride, qo, qo_stride, k.shape[1], kp, k_stride, ko, ko_stride)
+    kp, k_rows, Hkv, k_d, k_stride = _rows_of(k, dtype, gpu, "k")
+    if k_rows != rows or k_d != d:
+        _refuse("k", f"[{rows}, heads, {d}]", k)
+    q_out, qo, qo_stride = _place(q_out, q, rows, H, d, gpu, "out of q")
+    k_out, ko, ko_stride = _place(k_out, k, rows, Hkv, d, gpu, "out of k")
+    _on(gpu, call, code, rows, d, rope.c, pos, H, qp, q_stride, qo, qo_stride, Hkv, kp, k_stride, ko, ko_stride)
     return q_out, k_out
 
 
@@ -530,8 +533,9 @@ class PagedKVCache:
 
 def _paged_rows(call, cache, k, v, start, n, rows, row_start):
     gpu, B, i32 = cache.gpu, cache.B, torch.int32
-    kp, stride = _rows_arg(k, cache.row_dtype, None, cache.heads, cache.d, gpu, "k rows")
-    n_rows = k.shape[0]
+    kp, n_rows, heads, d, stride = _rows_of(k, cache.row_dtype, gpu, "k rows")
+    if heads != cache.heads or d != cache.d:
+        _refuse("k rows", f"[rows, {cache.heads}, {cache.d}]", k)
     if v.dtype is not k.dtype or v.get_device() != gpu or v.shape != k.shape or (v.stride() != k.stride() and n_rows > 1):
         _refuse("v rows", f"what the k rows are ({k.dtype} {tuple(k.shape)}, strides {k.stride()}, on {k.device})", v)
     vp = v.data_ptr()
@@ -580,9 +584,10 @@ def _attention_workspace(cache, B, H, max_kv_len):
 def eagle3_paged_attention(cache, q, kv_len, max_kv_len, scale=None, out=None, want_lse=False):
     """q [B, H, d] over each sequence's first kv_len[b] <= max_kv_len tokens; scale: 1 / sqrt(d) by default.  Returns out [B, H, d], with
     want_lse also the log of the softmax's sum, fp32 [B, H]."""
-    gpu, B, d, dtype, L = cache.gpu, cache.B, cache.d, cache.row_dtype, lib()
-    qp, stride = _rows_arg(q, dtype, B, None, d, gpu, "q")
-    H = q.shape[1]
+    gpu, B, dtype, L = cache.gpu, cache.B, cache.row_dtype, lib()
+    qp, n, H, d, stride = _rows_of(q, dtype, gpu, "q")
+    if n != B or d != cache.d:
+        _refuse("q", f"[{B}, heads, {cache.d}]", q)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         to = out.data_ptr()
