@@ -13,8 +13,8 @@
 // tile ahead of the products.  8-bit rows become bf16 by an exact conversion (a value row's scale multiplies its weight instead: a conversion takes two keys).
 //
 // Bound by bytes: 64 sequences of 512..2048 tokens, 32 heads of 128 over 8, bf16: 64.0 us, 5.2 TB/s (8 bits: 40.0 us, of which 4.8 join); one of 131071
-// under 64 heads in 8 bits 56.9 us, 5.2 TB/s and 5.6 us of joining; 256 of 1300 in bf16 237 us, 5.7 TB/s.  A tile of 128 dimensions is 8 score and 16 value products and some
-// 180 (bf16) or 230 (8 bits) vector instructions, 10 and 20 % of the time that its bytes take.  Two tiles of registers in flight in turn took 211 registers and 4 % longer than
+// under 64 heads in 8 bits 56.9 us, 5.2 TB/s and 5.6 us of joining; 256 of 1300 in bf16 237 us, 5.7 TB/s.  A tile of 128 dimensions is 8 score and 24 value products and some
+// 200 (bf16) or 250 (8 bits) vector instructions, 11 and 23 % of the time that its bytes take.  Two tiles of registers in flight in turn took 211 registers and 4 % longer than
 // one whose halves are asked for again as soon as they are used (150).
 #include <cfloat>
 
@@ -28,6 +28,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = PAGED_WAVES;
 constexpr float SLACK = 8.f;              // the running maximum moves when a score exceeds it by more than 2^8
+constexpr int PARTS = 3;                  // bf16 terms of a weight
 
 // What a kernel needs for its first loads comes in arguments of its own as well, which are in registers when it starts (one sequence of 4096 tokens 10.2 -> 9.8 us, of 128
 // 4.55 -> 4.46).
@@ -274,7 +275,7 @@ struct Walk {
       }
       if (16 * (m >> 2 & 1) + 4 * g + (m & 3) >= left) t.exps = 127;                // nor what lies in the place of an exponent
     }
-    u32x4 head[TILES], tail[TILES];
+    u32x4 part[TILES][PARTS];
     float w[TILES][E];
 #pragma unroll
     for (int r = 0; r < TILES; ++r) {
@@ -295,22 +296,29 @@ struct Walk {
         l[r] += w[r][e];
       }
       if constexpr (FP8) static_for<0, E>([&](auto e) { w[r][e] *= exp_scale(bcast16<8 + e>(t.exps)); });
-      // a weight as a head of 8 bits and a tail of 8 more; the tail of a weight above zero is above zero, so that an infinity stays one
+      // a weight as three bf16 terms of 8 bits each, all 24 of it.  With two, outputs were off by 3e-6 of their norm before they are rounded to bf16, and the difference of
+      // two equal weights by 2e-5 of them; with three 4e-7 and 1e-6, as any sum in 32 bits, in the same time (the cases above: 63.9 / 64.0, 39.5 / 39.5, 56.6 / 56.8 us).
+      // What is left behind a term is kept above zero, by 2^-24 of the term, so that an infinity times it stays one.
       if constexpr (!F32)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t w0 = __float_as_uint(w[r][2 * j]), w1 = __float_as_uint(w[r][2 * j + 1]);
-          head[r][j] = __builtin_amdgcn_perm(w1, w0, 0x07060302u);
-          tail[r][j] = pack_bf16x2(fmaf(__uint_as_float(w0 & 0xFFFF0000u), -0x1.fffffep-1f, w[r][2 * j]),
-                                   fmaf(__uint_as_float(w1 & 0xFFFF0000u), -0x1.fffffep-1f, w[r][2 * j + 1]));
+          float a = w[r][2 * j], b = w[r][2 * j + 1];
+#pragma unroll
+          for (int c = 0; c + 1 < PARTS; ++c) {
+            const uint32_t wa = __float_as_uint(a), wb = __float_as_uint(b);
+            part[r][c][j] = __builtin_amdgcn_perm(wb, wa, 0x07060302u);
+            a = fmaf(__uint_as_float(wa & 0xFFFF0000u), -0x1.fffffep-1f, a);
+            b = fmaf(__uint_as_float(wb & 0xFFFF0000u), -0x1.fffffep-1f, b);
+          }
+          part[r][PARTS - 1][j] = pack_bf16x2(a, b);
         }
     }
     auto product = [&](int i, const u32x4& a) {
 #pragma unroll
-      for (int r = 0; r < TILES; ++r) {
-        o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, head[r]), o[r][i], 0, 0, 0);
-        o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, tail[r]), o[r][i], 0, 0, 0);
-      }
+      for (int r = 0; r < TILES; ++r)
+#pragma unroll
+        for (int c = 0; c < PARTS; ++c)
+          o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, part[r][c]), o[r][i], 0, 0, 0);
     };
     if constexpr (F32) {
 #pragma unroll

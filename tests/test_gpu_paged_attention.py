@@ -422,3 +422,36 @@ def test_a_tree_is_verified_over_a_context_that_was_in_pages():
         got = verify(rk, rv)
         assert torch.equal(got, verify(qk, qv))
         assert dtype == "fp8" or torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("H", [4, 24])
+@pytest.mark.parametrize("bound", [300, 5000, 70000])
+def test_weights_keep_what_a_cancelling_sum_needs(dtype, H, bound):
+    """Dimension i is the difference of two weights w1, w2 that a factor of 2^(2^-13) parts, and nothing else.  Scores are exact in 32 bits (few significant bits,
+    and a scale that is 1 in units of log2), so a weight is off by one unit of exp2, 2^-23, and by what its split into bf16 terms loses: terms of 8, 8 and 8 bits
+    cut, cut and rounded leave 2^-24, and a first remainder is kept up by 2^-24 of its term, 2^-23 together.  Six additions to a sum of up to w1 are off by 2^-23 of
+    it at most.  In all (2 * 2 + 6) 2^-23 w1, and the output's rounding.  Weights of 16 bits would be off by up to 2 * 2^-16."""
+    d, n, scale = 128, 257, float(np.float32(np.log(2.0)))
+    assert np.float32(scale) * np.float32(1.4426950408889634) == 1
+    g = torch.Generator().manual_seed(H)
+    c, table = make_cache(dtype, 1, -(-bound // 16), 16, 1, d, g)
+    k, v = torch.zeros(n, 1, d), torch.zeros(n, 1, d)
+    k[0, 0, 0] = 1                                             # the maximum, without a value
+    coarse = -torch.randint(8, 16, (d, 3), generator=g) / 8
+    for i in range(2):
+        k[1 + i::2, 0, :3] = coarse
+        v[torch.arange(1 + i, n, 2), 0, torch.arange(d)] = 1.0 - 2 * i
+    k[2::2, 0, 3] = -1
+    q = torch.zeros(1, H, d)
+    q[0, :, 0] = 1
+    q[0, :, 1:3] = (0.1 + 0.4 * torch.rand(H, 2, generator=g)).bfloat16().float()
+    q[..., 3] = 2.0 ** -13
+    E.eagle3_paged_append(c, k.bfloat16().to(DEV), v.bfloat16().to(DEV), i32([0]).to(DEV))
+    out = E.eagle3_paged_attention(c, q.bfloat16().to(DEV), i32([n]).to(DEV), bound, scale=scale)[0].cpu().double()
+    assert torch.equal(_rows(c, "k")[table[0].long()[torch.arange(n) // 16] * 16 + torch.arange(n) % 16], k.double())
+    p = torch.softmax(scale * (q[0].double() @ k[:, 0].double().T), 1)
+    ref = p[:, 1::2] - p[:, 2::2]
+    tol = 10 * 2.0 ** -23 * p[:, 1::2]
+    tol = tol + 2.0 ** -8 * (ref + tol)
+    assert bool(((out - ref).abs() <= tol).all()), float(((out - ref).abs() / tol).max())
