@@ -537,7 +537,7 @@ def _paged_rows(call, cache, k, v, start, n, rows, row_start):
     kp, n_rows, heads, d, stride = _rows_of(k, cache.row_dtype, gpu, "k rows")
     if heads != cache.heads or d != cache.d:
         _refuse("k rows", f"[rows, {cache.heads}, {cache.d}]", k)
-    if v.dtype is not k.dtype or v.get_device() != gpu or v.shape != k.shape or (v.stride() != k.stride() and n_rows > 1):
+    if v.dtype is not k.dtype or v.get_device() != gpu or v.shape != k.shape or (v.stride() != k.stride() and _rows_of(v, k.dtype, gpu, "v rows")[4] != stride):
         _refuse("v rows", f"what the k rows are ({k.dtype} {tuple(k.shape)}, strides {k.stride()}, on {k.device})", v)
     vp = v.data_ptr()
     if rows is None:

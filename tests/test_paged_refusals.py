@@ -111,3 +111,35 @@ def test_the_binding_wants_tensors_on_a_gpu(L):
         E.PagedKVCache(pool, pool, table)
     with pytest.raises(ValueError):
         E.eagle3_rope(None, table, pool[0])
+
+
+@pytest.mark.parametrize("call", ["append", "read"])
+@pytest.mark.parametrize("rows", [1, 2])
+def test_values_lie_as_the_keys_do(L, monkeypatch, call, rows):
+    """The heads of a value row one behind the other, as those of a key row: of one row too.  (Tensors on the CPU, the launch replaced by a list.)"""
+    from types import SimpleNamespace
+    sent = []
+    monkeypatch.setattr(Bd, "_on", lambda gpu, call, *args: sent.append(args))
+    cache = SimpleNamespace(gpu=-1, B=1, row_dtype=torch.bfloat16, heads=8, d=128, c=None)
+    z = lambda *shape: torch.zeros(*shape, dtype=torch.bfloat16)
+    start = torch.zeros(1, dtype=torch.int32)
+    go = (lambda k, v: E.eagle3_paged_append(cache, k, v, start)) if call == "append" else (lambda k, v: E.eagle3_paged_read(cache, start, out=(k, v)))
+    k = z(rows, 8, 128)
+    bad = [z(rows, 24, 128)[:, ::3], z(rows, 128, 8).transpose(1, 2), z(1, 1, 128).expand(rows, 8, 128), z(1, 1, 1).expand(rows, 8, 128), z(rows, 8, 256)[..., ::2],
+           z(rows, 4, 128), z(rows + 1, 8, 128), z(rows, 8, 64), z(rows, 8, 128).float(), z(rows * 8, 128)]
+    for v in bad:
+        for pair in ((k, v), (v, k)):
+            with pytest.raises(ValueError):
+                go(*pair)
+    if rows > 1:                                              # one distance from row to row for both
+        with pytest.raises(ValueError):
+            go(k, z(rows, 16, 128)[:, :8])
+    assert not sent
+    # any distance for a single row, and for a single head's strides
+    packed = z(rows, 24, 128)
+    good = [(k, z(rows, 8, 128)), (packed[:, :8], packed[:, 16:])] + ([(k, packed[:, 8:16])] if rows == 1 else [])
+    for i, (k, v) in enumerate(good):
+        go(k, v)
+        assert sent[-1][6:8] == (k.data_ptr(), v.data_ptr()) and sent[-1][8:] == (rows, k.stride(0) if rows > 1 else 8 * 128)
+    cache.heads = 1
+    go(z(rows, 1, 128), z(rows, 128, 1).transpose(1, 2))
