@@ -494,15 +494,43 @@ def _rotate(call, rope, positions, q, k, out):
     return q_out, k_out
 
 
+class _Turned(torch.autograd.Function):
+    """A rotation for which gradients are wanted: its backward pass is the way back, whose own is the rotation."""
+
+    @staticmethod
+    def forward(ctx, call, back, rope, positions, q, k):
+        ctx.save_for_backward(positions)
+        ctx.turn = back, call, rope
+        return _rotate(call, rope, positions, q, k, None)
+
+    @staticmethod
+    def backward(ctx, dq, dk=None):
+        grads = _turn(*ctx.turn, ctx.saved_tensors[0], dq.contiguous(), None if dk is None else dk.contiguous(), None)
+        return None, None, None, None, *((grads, None) if dk is None else grads)
+
+
+def _turn(call, back, rope, positions, q, k, out):
+    wanted = q.requires_grad or (k is not None and k.requires_grad)
+    if out is not None:
+        wanted = wanted or any(t is not None and t.requires_grad for t in (out if isinstance(out, (tuple, list)) else (out,)))
+    if not wanted or not torch.is_grad_enabled():
+        return _rotate(call, rope, positions, q, k, out)
+    if out is not None:
+        _refuse("out", "None where gradients are recorded", out)
+    return _Turned.apply(call, back, rope, positions, q, k)
+
+
 def eagle3_rope(rope, positions, q, k=None, out=None):
     """q [rows, H, d] and k [rows, Hkv, d] (bf16 or fp32, rows any distance apart) turned to their positions (int32 [rows]).  `out`: where
-    to, e.g. (q, k) themselves; returns the rotated q, or (q, k).  Nothing is recorded for autograd: eagle3_rope_grad is its backward pass."""
-    return _rotate(lib().eagle3_rope, rope, positions, q, k, out)
+    to, e.g. (q, k) themselves; returns the rotated q, or (q, k).  Recorded for autograd where q or k requires a gradient, which `out` does not allow."""
+    L = lib()
+    return _turn(L.eagle3_rope, L.eagle3_rope_grad, rope, positions, q, k, out)
 
 
 def eagle3_rope_grad(rope, positions, dq, dk=None, out=None):
     """The gradients of eagle3_rope's q and k from those of its results."""
-    return _rotate(lib().eagle3_rope_grad, rope, positions, dq, dk, out)
+    L = lib()
+    return _turn(L.eagle3_rope_grad, L.eagle3_rope, rope, positions, dq, dk, out)
 
 
 _POOL_TYPES = {torch.bfloat16: EAGLE3_BF16, torch.float32: EAGLE3_FP32, torch.float8_e4m3fn: EAGLE3_FP8}
@@ -552,7 +580,7 @@ def _paged_rows(call, cache, k, v, start, n, rows, row_start):
 
 def eagle3_paged_append(cache, k_new, v_new, start, n_new=None, rows=None, row_start=None):
     """Writes k_new, v_new [n_rows, Hkv, d] behind the sequences' first start[b] tokens: n_new[b] rows each (None: `rows`, by default
-    n_rows / B), sequence b's from row row_start[b] (None: b * rows) on."""
+    n_rows / B), sequence b's from row row_start[b] (None: b * rows) on.  Nothing is recorded for autograd, here and in the calls below."""
     _paged_rows(lib().eagle3_paged_append, cache, k_new, v_new, start, n_new, rows, row_start)
 
 

@@ -203,3 +203,57 @@ def test_binding_refuses_what_does_not_fit():
         E.eagle3_rope(rope, pos, q[..., ::2])
     with pytest.raises(E.Eagle3Error):
         E.eagle3_rope(E.Rope(128, 1e4, device=DEV), pos, q)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("alone", [False, True])
+def test_gradients_are_recorded_where_they_are_wanted(inter, alone):
+    """The gradients of leaves through the call itself are the bits of eagle3_rope_grad, and those of the gradients' gradients of eagle3_rope."""
+    rows, H, Hkv, d, rot = 9, 4, 2, 64, 48
+    g = torch.Generator().manual_seed(7)
+    rope = E.Rope(rot, 1e4, interleaved=inter, amplitude=1.5, device=DEV)
+    pos = torch.randint(0, 4096, (rows,), generator=g, dtype=torch.int32).to(DEV)
+    heads = (H,) if alone else (H, Hkv)
+    x = [torch.randn(rows, h, d, generator=g).to(DEV).requires_grad_() for h in heads]
+    w = [torch.randn(rows, h, d, generator=g).to(DEV).requires_grad_() for h in heads]
+    tup = lambda y: y if isinstance(y, tuple) else (y,)
+    y = tup(E.eagle3_rope(rope, pos, *x))
+    with torch.no_grad():
+        plain, back = tup(E.eagle3_rope(rope, pos, *x)), tup(E.eagle3_rope_grad(rope, pos, *w))
+    assert all(torch.equal(a, b) and a.requires_grad and not b.requires_grad for a, b in zip(y, plain))
+    dx = torch.autograd.grad(y, x, w, create_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(dx, back))
+    u = [torch.randn_like(t) for t in x]
+    with torch.no_grad():
+        again = tup(E.eagle3_rope(rope, pos, *u))
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(dx, w, u), again))
+    # expanded gradients (of a sum); and of one of the two tensors only, the other's result unused
+    sum(t.sum() for t in tup(E.eagle3_rope(rope, pos, *x))).backward()
+    ones = tup(E.eagle3_rope_grad(rope, pos, *[torch.ones_like(t) for t in x]))
+    assert all(torch.equal(t.grad, o) for t, o in zip(x, ones))
+    if not alone:
+        x[0].grad = None
+        q, _ = E.eagle3_rope(rope, pos, x[0], x[1].detach())
+        q.backward(w[0].detach())
+        assert torch.equal(x[0].grad, back[0])
+    # positions that move on before the backward pass would give other gradients
+    y = tup(E.eagle3_rope(rope, pos, *x))
+    pos += 1
+    with pytest.raises(RuntimeError):
+        y[0].sum().backward()
+
+
+def test_results_are_not_written_over_where_gradients_are_recorded():
+    rope = E.Rope(64, 1e4, device=DEV)
+    q, pos = torch.ones(3, 2, 64, device=DEV), torch.arange(3, dtype=torch.int32, device=DEV)
+    leaf = q.clone().requires_grad_()
+    product = leaf * 2
+    for call in (E.eagle3_rope, E.eagle3_rope_grad):
+        for x, k, out in ((product, None, product), (q, None, leaf), (q, product, (None, product)), (q, product, (q, None))):
+            with pytest.raises(ValueError):
+                call(rope, pos, x, k, out=out)
+    with torch.no_grad():
+        want = E.eagle3_rope(rope, pos, product)
+        assert E.eagle3_rope(rope, pos, product, out=product) is product and torch.equal(product, want)
+    x = q.clone()
+    assert E.eagle3_rope(rope, pos, x, out=x) is x and not x.requires_grad
