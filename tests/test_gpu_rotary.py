@@ -257,3 +257,32 @@ def test_results_are_not_written_over_where_gradients_are_recorded():
         assert E.eagle3_rope(rope, pos, product, out=product) is product and torch.equal(product, want)
     x = q.clone()
     assert E.eagle3_rope(rope, pos, x, out=x) is x and not x.requires_grad
+
+
+# A wavefront has up to 8192 / rows (at least one) parts of a row's pieces and takes 256 of them a round, 512 single elements: 584 pieces in three rounds (bf16) or
+# 1168 in five, 1168 or 2336 between neighbours, 4891 elements in ten; 3000 rows in two parts of 320 or 640; rows whose heads
+# are copied by half
+MANY_ROUNDS = [(4100, 64, 9, 128, 128, False), (4100, 64, 9, 128, 128, True), (4100, 64, 9, 128, 122, False), (4100, 64, 9, 128, 122, True), (3000, 64, 9, 128, 128, False),
+               (4097, 64, 9, 128, 64, False)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,H,Hkv,d,rot,inter", MANY_ROUNDS)
+def test_many_rows_of_many_heads(dtype, rows, H, Hkv, d, rot, inter):
+    """The bits of 250 rows at a time, whose pieces lie within one round; some rows against the formula; in place too."""
+    g = torch.Generator(device=DEV).manual_seed(rows + rot)
+    rope = E.Rope(rot, 5e5, interleaved=inter, scaling="linear", amplitude=1.25, device=DEV, factor=8.0)
+    x = torch.randn(rows, H + Hkv, d, generator=g, device=DEV).to(dtype)
+    q, k = x[:, :H], x[:, H:]
+    pos = torch.randint(-50, 131072, (rows,), generator=g, device=DEV, dtype=torch.int32)
+    for call, sign in ((E.eagle3_rope, 1), (E.eagle3_rope_grad, -1)):
+        got = call(rope, pos, q, k)
+        few = [call(rope, pos[i:i + 250], q[i:i + 250], k[i:i + 250]) for i in range(0, rows, 250)]
+        for i in range(2):
+            assert torch.equal(got[i], torch.cat([f[i] for f in few]))
+        at = [0, 1, 2, 3, rows // 2, rows - 2, rows - 1]
+        for y, t in zip(got, (q, k)):
+            _check(y[at], t[at], (rot, 5e5, inter, "linear", 1.25), pos[at], sign)
+        both = x.clone()
+        call(rope, pos, both[:, :H], both[:, H:], out=(both[:, :H], both[:, H:]))
+        assert torch.equal(both[:, :H], got[0]) and torch.equal(both[:, H:], got[1])
