@@ -455,3 +455,34 @@ def test_weights_keep_what_a_cancelling_sum_needs(dtype, H, bound):
     tol = 10 * 2.0 ** -23 * p[:, 1::2]
     tol = tol + 2.0 ** -8 * (ref + tol)
     assert bool(((out - ref).abs() <= tol).all()), float(((out - ref).abs() / tol).max())
+
+
+# a workgroup to a sequence, ranges, and two products of each operand in either way
+@pytest.mark.parametrize("H,Hkv,B,bound", [(8, 2, 2, 704), (8, 2, 2, 5000), (48, 1, 100, 704), (48, 1, 2, 40000)])
+@pytest.mark.parametrize("page", [1, 16, 100])
+@pytest.mark.parametrize("n", [1, 40, 64, 700])
+def test_what_is_behind_a_sequence_in_8_bits_does_not_reach_it(H, Hkv, B, bound, page, n):
+    """NaN codes and the largest ones under exponent bytes of 0, 254 and 255 (an infinite scale) in every slot that no visible token has."""
+    g = torch.Generator().manual_seed(n + page)
+    c, table = make_cache("fp8", B, -(-n // page) + 2, page, Hkv, 128, g)
+    for e in (c.k_exp, c.v_exp):
+        e.clamp_(117, 120)
+    wide = torch.zeros(B, max(-(-bound // page), table.shape[1]), dtype=torch.int32)
+    wide[:, :table.shape[1]] = table
+    c = E.PagedKVCache(c.k, c.v, wide.to(DEV), c.k_exp, c.v_exp)
+    seen = torch.zeros(c.k.shape[0], page, dtype=torch.bool)
+    pos = torch.arange(n)
+    seen[table[0].long()[pos // page], pos % page] = True
+    unseen = ~seen.to(DEV)
+    q = torch.randn(B, H, 128, generator=g).bfloat16().to(DEV)
+    lens = [n] + [0] * (B - 1)
+    want = E.eagle3_paged_attention(c, q, i32(lens).to(DEV), bound, want_lse=True)
+    _check(c, wide, q, lens, *want)
+    for code in (0x7F, 0xFF, 0x7E, 0xFE):
+        for exp in (0, 254, 255):
+            for t in (c.k, c.v):
+                t.view(torch.uint8)[unseen] = code
+            for t in (c.k_exp, c.v_exp):
+                t[unseen] = exp
+            got = E.eagle3_paged_attention(c, q, i32(lens).to(DEV), bound, want_lse=True)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (code, exp)
