@@ -317,7 +317,8 @@ int eagle3_rope_grad(int32_t dtype, int32_t rows, int32_t head_dim, const eagle3
 /* One layer's cache in pages of a pool shared by B sequences: token p of sequence b lies in slot
  * page_table[b][p / page_size] * page_size + p % page_size.  The arrays are those of a cache of n_pages * page_size slots as the
  * calls above have it.  EAGLE3_FP8 holds bf16 rows in 8 bits: the row of a (slot, KV head) is head_dim codes and one exponent byte
- * x, and a code c stands for the value e4m3(c) * 2^(x - 127), which bf16 holds exactly; x is 1..254. */
+ * x, and a code c stands for the value e4m3(c) * 2^(x - 127).  What eagle3_paged_append writes, x of 17..247 and with 247 no code
+ * above 240 in magnitude, bf16 holds exactly; a cache filled by other means has to keep to these where it is read. */
 typedef struct {
   void *k, *v;                            /* DEVICE [n_pages, page_size, n_kv_heads, head_dim], at multiples of 16 bytes       */
   uint8_t *k_exp, *v_exp;                 /* DEVICE [n_pages, page_size, n_kv_heads]; EAGLE3_FP8 only, else NULL               */
@@ -360,6 +361,7 @@ int eagle3_paged_read(const eagle3_paged_kv* kv, int32_t B, int32_t rows, const 
  *   workspace  DEVICE, 256-byte aligned, of the bytes that the next call tells for the same sizes; NULL if these are 0.  Its content
  *              need not be kept or cleared between calls; calls that may overlap in time need one each.
  * Page numbers are clamped into the pool.  A sequence's infinite or NaN keys and values make its results NaN or infinite, no other's.
+ * Sums are formed with weights of up to 2^8: they stay finite where kv_len times the largest magnitude of a value is below 2^120.
  * Requires n_heads a multiple of n_kv_heads and B <= 65535. */
 int eagle3_paged_attention(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads, const void* q, int64_t q_stride, const int32_t* kv_len,
                            int32_t max_kv_len, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,

@@ -486,3 +486,34 @@ def test_what_is_behind_a_sequence_in_8_bits_does_not_reach_it(H, Hkv, B, bound,
                 t[unseen] = exp
             got = E.eagle3_paged_attention(c, q, i32(lens).to(DEV), bound, want_lse=True)
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (code, exp)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("up", [105, -99])
+@pytest.mark.parametrize("bound", [4000, 700])
+def test_values_of_any_magnitude(dtype, up, bound):
+    """Values times a power of two give results times it.  Up: bit for bit as long as the number of tokens times the largest, 4 * 2^105, is below 2^120; scores rise by
+    less than 2^8 within a workgroup's reach, so that weights are as large as they may be.  Down: weights times an 8-bit row's scale, at least 2^-8 * 2^-107, are held in
+    bf16 terms of multiples of 2^-133, which takes less than 2^-18 of a weight (weights of 2^-8 count 1 / 256); the output's two roundings may fall apart by a step, 2^-7."""
+    n, d = bound, 128
+    g = torch.Generator().manual_seed(bound)
+    k = torch.zeros(n, 1, d)
+    k[:, 0, 0] = torch.linspace(0, 7 * math.log(2.0), n)
+    v = torch.randn(n, 1, d, generator=g).clamp(-4, 4)
+    q = torch.zeros(1, 4, d)
+    q[..., 0] = d ** 0.5
+    q = q.to(ROW[dtype]).to(DEV)
+    outs = []
+    for scale in (1.0, 2.0 ** up):
+        c, table = make_cache(dtype, 1, -(-n // 16), 16, 1, d, torch.Generator().manual_seed(5))
+        E.eagle3_paged_append(c, k.to(ROW[dtype]).to(DEV), (v * scale).to(ROW[dtype]).to(DEV), i32([0]).to(DEV))
+        out, lse = E.eagle3_paged_attention(c, q, i32([n]).to(DEV), n, want_lse=True)
+        if scale == 1.0:
+            _check(c, table, q, [n], out, lse)
+        outs.append(out.double())
+    assert bool(torch.isfinite(outs[1]).all())
+    if up > 0:
+        assert torch.equal(outs[1], outs[0] * 2.0 ** up)
+    else:
+        err = (outs[1] * 2.0 ** -up - outs[0]).abs()
+        assert bool((err <= 2.0 ** -7 * outs[0].abs() + 2.0 ** -18 * 4).all()), float(err.max())
