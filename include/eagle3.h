@@ -292,7 +292,8 @@ typedef struct {
  *   LINEAR  f_i / factor
  *   PARTS   by how often a pair turns within original_len positions: f_i / factor up to `low` turns, f_i from `high` turns on, and
  *           between them f_i (w + (1 - w) / factor) with w = (original_len f_i - low) / (high - low)
- * Requires theta > 0, even rot_dim >= 2; LINEAR, PARTS: factor > 0; PARTS: original_len > 0 and low < high; all finite. */
+ * Requires theta > 0, even rot_dim >= 2; LINEAR, PARTS: factor > 0; PARTS: original_len > 0 and low < high; all finite,
+ * and the turns of 2^31 positions too. */
 int eagle3_rope_turns(int32_t rot_dim, double theta, int32_t scaling, double factor, double low, double high, double original_len,
                       double* out);
 

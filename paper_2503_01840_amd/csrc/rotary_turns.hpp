@@ -10,14 +10,17 @@ inline bool rope_turns(int rot, double theta, int scaling, double factor, double
   if (scaling >= 1 && (!(factor > 0) || !std::isfinite(factor))) return false;
   if (scaling == 2 && (!(original_len > 0) || !std::isfinite(original_len) || !(low < high) || !std::isfinite(high - low))) return false;
   const double two_pi = 6.283185307179586476925286766559;
-  for (int i = 0; i < rot / 2; ++i) {
+  auto turns = [&](int i) {
     double f = std::pow(theta, -2.0 * i / rot) / two_pi;
     if (scaling == 1) f /= factor;
     if (scaling == 2) {
       const double w = std::min(1.0, std::max(0.0, (original_len * f - low) / (high - low)));
       f *= w + (1 - w) / factor;
     }
-    out[i] = f;
-  }
+    return f;
+  };
+  for (int i = 0; i < rot / 2; ++i)
+    if (!(turns(i) < 0x1p992)) return false;                // position times turns has to be a number, for any int32 position
+  for (int i = 0; i < rot / 2; ++i) out[i] = turns(i);
   return true;
 }

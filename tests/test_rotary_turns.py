@@ -74,3 +74,12 @@ def test_turns_need_a_place(L):
         E.Rope(63, 1e4)
     with pytest.raises(ValueError):
         E.Rope(64, 1e4, device="cpu")
+
+
+@pytest.mark.parametrize("args", [(64, 1e4, 1, 5e-324, 1, 4, 8192), (64, 1e4, 2, 5e-324, 1, 4, 8192), (128, 5e-324, 0, 1, 1, 4, 8192), (64, 1e-300, 1, 1e-100, 1, 4, 8192),
+                                  (2, 1e4, 1, 1e-300, 1, 4, 8192)])
+def test_turns_that_no_number_holds_are_refused(L, args):
+    """Parameters each in range whose turns are not, or not times the farthest position: every rotated value would be NaN."""
+    out = torch.full((args[0] // 2,), 7.0, dtype=torch.float64)
+    assert L.eagle3_rope_turns(*args, out.data_ptr()) == -2
+    assert bool((out == 7).all())
