@@ -12,8 +12,8 @@
 // No tile passes through LDS, no wavefront waits for another while it walks, and a page may end anywhere: pages are looked up one tile ahead of the loads, which are one
 // tile ahead of the products.  8-bit rows become bf16 by an exact conversion (a value row's scale multiplies its weight instead: a conversion takes two keys).
 //
-// Bound by bytes: 64 sequences of 512..2048 tokens, 32 heads of 128 over 8, bf16: 64.0 us, 5.2 TB/s (8 bits: 40.0 us, of which 4.8 join); one of 131071
-// under 64 heads in 8 bits 56.9 us, 5.2 TB/s and 5.6 us of joining; 256 of 1300 in bf16 237 us, 5.7 TB/s.  A tile of 128 dimensions is 8 score and 24 value products and some
+// Bound by bytes: 64 sequences of 512..2048 tokens, 32 heads of 128 over 8, bf16: 64.0 us, 5.2 TB/s (8 bits: 40.0 us, of which 5 join); one of 131071
+// under 64 heads in 8 bits 56.9 us, 5.2 TB/s and 5.2 us of joining; 256 of 1300 in bf16 237 to 253 us by box, 5.4 to 5.7 TB/s.  A tile of 128 dimensions is 8 score and 24 value products and some
 // 200 (bf16) or 250 (8 bits) vector instructions, 11 and 23 % of the time that its bytes take.  Two tiles of registers in flight in turn took 211 registers and 4 % longer than
 // one whose halves are asked for again as soon as they are used (150).
 #include <cfloat>
@@ -297,7 +297,8 @@ struct Walk {
       }
       if constexpr (FP8) static_for<0, E>([&](auto e) { w[r][e] *= exp_scale(bcast16<8 + e>(t.exps)); });
       // a weight as three bf16 terms of 8 bits each, all 24 of it.  With two, outputs were off by 3e-6 of their norm before they are rounded to bf16, and the difference of
-      // two equal weights by 2e-5 of them; with three 4e-7 and 1e-6, as any sum in 32 bits, in the same time (the cases above: 63.9 / 64.0, 39.5 / 39.5, 56.6 / 56.8 us).
+      // two equal weights by 2e-5 of them; with three 4e-7 and 1e-6, as any sum in 32 bits, in the same time where keys come from memory (the cases above: 63.9 / 64.0, 39.5 / 39.5, 56.6 / 56.8 us; 8 bits of 64
+      // dimensions 26.4 / 27.8, 32 heads over one, 100 sequences of 300..700 in 8 bits 12.8 / 13.6).
       // What is left behind a term is kept above zero, by 2^-24 of the term, so that an infinity times it stays one.
       if constexpr (!F32)
 #pragma unroll

@@ -13,18 +13,23 @@ struct PagedSplit {
   int ranges;                             // into how many all sequences' keys are divided; 0: a workgroup per sequence and unit, one launch
   bool team;                              // a range of a unit to a workgroup, else to a wavefront
 };
-// A launch that knows only a bound of the lengths.  Times in us, whole / team / wavefronts, 32 heads of 128 over 8:
-//   A CU draws some 50 GB/s, so a whole context goes to one workgroup where it is short: one sequence of 256 tokens 5.7 / 6.9 / 9.1, of 512
-//   7.8 / 7.1 / 9.7, of 768 10.8 / 8.2 / 10.5, of 2048 23.5 / 9.7 / 11.6 (bf16).  The second launch that parts need costs the host 4 us more, so up to 768.
-//   Where sequences fill the chip (the longest begin first) the second launch costs more than uneven lengths: 32 of 500..1024 tokens 24.9 / 28.3 / 29.1, 64 of
-//   300..1024 38.1 / 42.9 / 42.5, 48 of 512..2048 53.6 / 56.0 / 55.8, 64 of them 65.2 / 70.1 / 69.4, in fp32 117 / 120 / 128; but 32 of 500..4096 75.2 / 64.5 / 62.8,
-//   and where a head's row is one memory line only, 64 of 512..2048 in 8 bits 45.9 / 45.9 / 42.0, in bf16 with 64 dimensions 43.3 / 44.7 / 37.8.
+// A launch that knows only a bound of the lengths.  Times in us, in captured graphs, whole / team / wavefronts, 32 heads of 128 over 8:
+//   A CU draws some 50 GB/s, so a whole context goes to one workgroup where it is short: one sequence of 256 tokens 5.7 / 6.8 / 11.0, of 512
+//   7.9 / 7.0 / 11.3, of 768 10.7 / 8.4 / 12.9, of 2048 23.0 / 8.6 / 12.6 (bf16).  The second launch that parts need costs the host 4 us more, so up to 768 (a graph
+//   pays no such cost, and is up to 2.4 us slower than in parts from 513 on).
+//   Where sequences fill the chip (the longest begin first) the second launch costs more than uneven lengths: 32 of 500..1024 tokens 24.7 / 27.4 / 28.6, 64 of
+//   300..1024 38.3 / 42.3 / 41.9, 48 of 512..2048 53.5 / 55.7 / 54.5, 64 of them 65.1 / 71.3 / 70.9, in fp32 117 / 119 / 127; but 32 of 500..4096 75.4 / 64.1 / 63.7,
+//   and where a head's row is one memory line only, 64 of 512..2048 in 8 bits 46.5 / 45.7 / 41.6, in bf16 with 64 dimensions 43.3 / 44.2 / 38.7.
+//   Beyond 2048 tokens it depends on the lengths: 40 (320 groups) of 512..3000 62.3 / 59.9 / 60.7, of 512..4096 84.2 / 78.0 / 75.9; 48 (384) of 512..4096 90.9 / 91.4 / 91.3, in fp32 of
+//   512..3000 123 / 123 / 131; 64 (512) of 512..3000 89.1 / 93.2 / 93.4, of 512..4096 115 / 119 / 118; 128 of them 225 / 229 / 225.
 //   A wavefront with a range of its own has no exchange at the end and, with eight units, reads whole rows together with its neighbours, but needs a long range and
-//   leaves more parts to join: 131071 tokens in 8 bits under 64 heads 62.4 (team) / 57.3, 256 of 1300 in bf16 259 / 237; 8 of 4000..8192 44.6 / 45.1, 16 of
-//   1000..2048 in fp32 41.9 / 46.2, one of 16384 under 64 heads 19.8 / 22.7; 24 heads over one, 19 of up to 103066 in 8 bits 60.1 / 68.6.
-// More than 16 query heads to a KV head: 32 of them to a wavefront, as two products of each operand, but for few keys, which leave CUs idle (16 / 32 heads, us: that case
-// 79.1 / 60.1, 64 over one, 16 of 4096..8192 in bf16 35.9 / 28.2, 64 of 512..2048 under 24 22.4 / 21.9; 4 of 100..700 10.2 / 12.4), and not with fp32 caches,
-// whose operands leave no registers for it.
+//   leaves more parts to join: 131071 tokens in 8 bits under 64 heads 63.0 (team) / 57.2, 256 of 1300 in bf16 255 / 245; 8 of 4000..8192 44.0 / 46.1, 16 of
+//   1000..2048 in fp32 42.5 / 46.8, one of 16384 under 64 heads 19.8 / 22.8; 24 heads over one, 19 of up to 103066 in 8 bits 61.7 / 70.2.
+//   Beyond 1024 sequences every wavefront would look through them all: 1025 of 100..2000 823 / 858 / 808, 1500 of up to 1500 under 8 heads over 2 226 / 247 / 249, 2000 of 100..3000
+//   so in 8 bits with 64 dimensions 226 / 267 / 207.
+// More than 16 query heads to a KV head: 32 of them to a wavefront, as two products of each operand, but for few keys, which leave CUs idle (16 / 32 heads, us, beside what a copy of as many
+// bytes takes: that case 79.2 / 60.1, 50.9; 64 over one, 16 of 4096..8192 in bf16 35.9 / 28.0, 10.2; 64 of 512..2048 under 24 21.3 / 19.5, 8.6; 4 of 100..700 10.4 / 12.9, 0.2), and not with
+// fp32 caches, whose operands leave no registers for it.
 // row_bytes: of a head's row in the cache.
 inline PagedSplit paged_split(int B, int H, int Hkv, int row_bytes, bool fp32, int max_len) {
   const int G = H / Hkv;
