@@ -286,3 +286,37 @@ def test_many_rows_of_many_heads(dtype, rows, H, Hkv, d, rot, inter):
         both = x.clone()
         call(rope, pos, both[:, :H], both[:, H:], out=(both[:, :H], both[:, H:]))
         assert torch.equal(both[:, :H], got[0]) and torch.equal(both[:, H:], got[1])
+
+
+def test_a_captured_step_with_its_gradients_replays():
+    """Forward and backward pass in one graph, replayed with other inputs and positions, against the eager calls."""
+    rows, H, Hkv, d = 65, 4, 2, 64
+    g = torch.Generator().manual_seed(8)
+    rope = E.Rope(d, 1e4, device=DEV)
+    pos = torch.arange(rows, dtype=torch.int32, device=DEV)
+    x = [torch.randn(rows, h, d, generator=g).to(DEV).requires_grad_() for h in (H, Hkv)]
+    w = [torch.randn(rows, h, d, generator=g).to(DEV) for h in (H, Hkv)]
+
+    def step():
+        y = E.eagle3_rope(rope, pos, *x)
+        return [t.detach() for t in y], torch.autograd.grad(y, x, w)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, dx = step()
+    for i in range(4):
+        with torch.no_grad():
+            for t in x + w:
+                t.copy_(torch.randn(t.shape, generator=g))
+            pos += 100
+            want, grads = E.eagle3_rope(rope, pos, *x), E.eagle3_rope_grad(rope, pos, *w)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(list(y) + list(dx), list(want) + list(grads))), i
+        (torch.randn(1000, device=DEV) * 2).sum()
