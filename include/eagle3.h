@@ -369,6 +369,92 @@ int eagle3_paged_attention(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads
                            eagle3_stream stream);
 int eagle3_paged_attention_workspace(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads, int32_t max_kv_len, size_t* bytes);
 
+/* ---- the ends of a layer stack: embeddings, norms, distillation ---------------------------------
+ * For programs that train a draft model around the calls above (its layer is a norm of embeddings, a norm of features, attention, and logits that are
+ * taught by the target's), and for layers of a program's own.  No call needs a context.  Types are EAGLE3_BF16 and EAGLE3_FP32 throughout; sums are
+ * formed in 32 bits, results rounded once.  No result depends on the order in which workgroups run.  Rows lie `stride` elements apart (at least their
+ * length, below 2^40) and may start at any multiple of their type's size; rows at multiples of 16 bytes are the fast ones.  Outputs do not overlap
+ * inputs except where that is said.  A workspace is DEVICE memory, 256-byte aligned, of the bytes that the call's _workspace tells for the same sizes;
+ * its content need not be kept or cleared between calls, and calls that may overlap in time need one each. */
+
+/* Rows of an embedding table, times a factor: out[r] = scale * table[tokens[r]].  Tokens outside 0..vocab-1 are padding: rows of zeros.
+ *   dtype, out_dtype  of the table [vocab, dim] (dense) and of out [rows, dim]
+ * Requires 1 <= rows < 2^24, 1 <= dim <= 65536, vocab >= 1. */
+int eagle3_embed(int32_t dtype, int32_t rows, int32_t dim, int32_t vocab, const void* table, const int32_t* tokens, float scale,
+                 int32_t out_dtype, void* out, int64_t out_stride, eagle3_stream stream);
+
+/* The table's gradient: d_table[v] = scale * the sum over the rows r with tokens[r] = v of dy[r]; rows of tokens that do not occur are zeros.  With
+ * `accumulate` it is added to what d_table holds, and rows of other tokens are not touched (nor read).  The sum of a token's rows is formed in an
+ * order that the tokens alone decide.
+ *   dtype, out_dtype  of dy [rows, dim] and of d_table [vocab, dim] (dense)
+ * Requires 1 <= rows < 2^22, 1 <= dim <= 65536, 1 <= vocab < 2^27. */
+int eagle3_embed_grad(int32_t dtype, int32_t rows, int32_t dim, int32_t vocab, const void* dy, int64_t dy_stride, const int32_t* tokens, float scale,
+                      int32_t accumulate, int32_t out_dtype, void* d_table, void* workspace, size_t workspace_bytes, eagle3_stream stream);
+int eagle3_embed_grad_workspace(int32_t rows, int32_t dim, int32_t vocab, size_t* bytes);
+
+/* The residual stream and its norm: h = x + residual, out = gain * h / sqrt(mean(h^2) + eps), from the sum before it is rounded to the stream's type.
+ *   x, x_dtype            [rows, dim]: what a layer's branch gives; without residual the stream itself (h = x)
+ *   residual, sum_out     [rows, dim] of sum_dtype, EAGLE3_FP32 or x_dtype; sum_out gets h and may be residual itself with the same stride.  Both NULL: no sum
+ *   gain, gain_dtype      [dim]
+ *   out, out_dtype        [rows, dim]; may be x itself with the same type and stride
+ * Requires 1 <= rows < 2^24, 1 <= dim <= 16384, eps >= 0. */
+int eagle3_add_norm(int32_t rows, int32_t dim, int32_t x_dtype, const void* x, int64_t x_stride, int32_t sum_dtype, const void* residual,
+                    int64_t residual_stride, void* sum_out, int64_t sum_stride, int32_t gain_dtype, const void* gain, float eps, int32_t out_dtype,
+                    void* out, int64_t out_stride, eagle3_stream stream);
+
+/* The same with the norm in 8 bits, as products of 8-bit rows take it: e4m3 codes c and fp32 scales s of groups of columns, a value being s * c.  A group's
+ * scale is its largest finite magnitude / 448, at least 2^-100; codes are rounded to nearest even, infinities and NaN stored as NaN.
+ *   group    columns to a scale: 128, or 0 for one scale a row; the last group of a row may be shorter
+ *   codes    [rows, dim], codes_stride bytes apart;  scales  fp32 [rows, ceil(dim / 128)] or [rows, 1], dense */
+int eagle3_add_norm_codes(int32_t rows, int32_t dim, int32_t x_dtype, const void* x, int64_t x_stride, int32_t sum_dtype, const void* residual,
+                          int64_t residual_stride, void* sum_out, int64_t sum_stride, int32_t gain_dtype, const void* gain, float eps, int32_t group,
+                          uint8_t* codes, int64_t codes_stride, float* scales, eagle3_stream stream);
+
+/* The gradient of eagle3_add_norm, from that of out (dy) and, where the sum is used further on, that of the sum (dh):
+ *   d_sum = dh + r (gain dy - h r^2 mean(gain dy h)),  r = 1 / sqrt(mean(h^2) + eps);   d_gain = sum over rows of dy h r
+ * d_sum is the gradient of x and of residual alike.
+ *   h, dh, d_sum   [rows, dim] of sum_dtype; dh may be NULL (no further use) or d_sum itself with the same stride; d_sum may be NULL if dx is not
+ *   dy, dy_dtype   [rows, dim], as out was
+ *   dx, x_dtype    [rows, dim] or NULL: d_sum once more, in the type of x
+ *   d_gain         [dim] of gain_dtype, or NULL
+ * Sizes as above. */
+int eagle3_add_norm_grad(int32_t rows, int32_t dim, int32_t dy_dtype, const void* dy, int64_t dy_stride, int32_t sum_dtype, const void* h,
+                         int64_t h_stride, const void* dh, int64_t dh_stride, int32_t gain_dtype, const void* gain, float eps, void* d_sum,
+                         int64_t d_sum_stride, int32_t x_dtype, void* dx, int64_t dx_stride, void* d_gain, void* workspace, size_t workspace_bytes,
+                         eagle3_stream stream);
+int eagle3_add_norm_grad_workspace(int32_t rows, int32_t dim, size_t* bytes);
+
+/* What a teacher says of every position: its k largest logits, or any k of them.  Entry j of row r is a token of the student's vocabulary, ids[r][j], or, with
+ * t2d, one of the teacher's that stands for t2d[ids[r][j]].  Entries that are none of the student's (outside either vocabulary, or mapped to a negative id) take
+ * no part.  The weights of the others are p_j = exp(z_j / T) / their sum, or with lse exp(z_j / T - lse[r]), the teacher's own probabilities, of which what is
+ * missing from 1 is left out.  A token that occurs twice has the sum of its weights. */
+typedef struct {
+  const int32_t* ids;       /* DEVICE [rows, k]                                                                */
+  const float* values;      /* DEVICE fp32 [rows, k]: logits z; -infinity: weight 0                            */
+  const float* lse;         /* DEVICE fp32 [rows]: log of the sum of exp(z / T) over the teacher's whole vocabulary, or NULL */
+  const int32_t* t2d;       /* DEVICE [n_t2d]: the student's id of a teacher's token, negative: none; or NULL  */
+  int32_t n_t2d, k;         /* 1 <= k <= 1024                                                                  */
+  float temperature;        /* T > 0, of the teacher and of the student                                        */
+} eagle3_teacher;
+
+/* Distillation: loss[r] = - sum_j p_j log softmax(logits[r] / T)[id_j], and its gradient d_logits[r][v] = dloss[r] / T (P softmax(logits[r] / T)[v] - p_v) with
+ * P the sum of the weights and p_v those of token v.  Rows without weights (no entry that counts, all weights zero) have loss 0 and gradient 0, rows
+ * whose dloss is 0 gradient 0, whatever their logits are.
+ *   logits, dtype  [rows, vocab], logits_stride elements apart;   loss  fp32 [rows]
+ *   stats          fp32 [rows, 2]: a row's largest logit m and the sum of exp((x - m) / T), what the gradient needs of it; may be NULL
+ *   dloss          DEVICE fp32 [rows]
+ *   d_logits       [rows, vocab] of dtype; may be logits itself with the same stride
+ * eagle3_distill_step gives loss and gradient of the same logits in one call.  eagle3_distill_grad needs no workspace.
+ * Requires 1 <= rows < 2^24, 1 <= vocab < 2^27. */
+int eagle3_distill(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t logits_stride, const eagle3_teacher* teacher, float* loss,
+                   float* stats, void* workspace, size_t workspace_bytes, eagle3_stream stream);
+int eagle3_distill_grad(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t logits_stride, const eagle3_teacher* teacher,
+                        const float* stats, const float* dloss, void* d_logits, int64_t d_logits_stride, eagle3_stream stream);
+int eagle3_distill_step(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t logits_stride, const eagle3_teacher* teacher,
+                        const float* dloss, float* loss, void* d_logits, int64_t d_logits_stride, void* workspace, size_t workspace_bytes,
+                        eagle3_stream stream);
+int eagle3_distill_workspace(int32_t rows, int32_t vocab, size_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

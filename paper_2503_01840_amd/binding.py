@@ -19,7 +19,8 @@ EXPORTS = ["eagle3_create", "eagle3_destroy", "eagle3_workspace_bytes", "eagle3_
            "eagle3_fuse_features", "eagle3_draft_expand",
            "eagle3_tree_verify", "eagle3_tree_verify_layers", "eagle3_accept", "eagle3_accept_static", "eagle3_commit", "eagle3_prefill", "eagle3_draft_chain", "eagle3_ttt_attention",
            "eagle3_rope_turns", "eagle3_rope", "eagle3_rope_grad", "eagle3_paged_append", "eagle3_paged_read", "eagle3_paged_attention",
-           "eagle3_paged_attention_workspace"]
+           "eagle3_paged_attention_workspace", "eagle3_embed", "eagle3_embed_grad", "eagle3_embed_grad_workspace", "eagle3_add_norm", "eagle3_add_norm_codes",
+           "eagle3_add_norm_grad", "eagle3_add_norm_grad_workspace", "eagle3_distill", "eagle3_distill_grad", "eagle3_distill_step", "eagle3_distill_workspace"]
 
 
 class Config(C.Structure):
@@ -59,6 +60,10 @@ class RopeSpec(C.Structure):
 class PagedKV(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_exp", "v_exp", "page_table")] + \
                [(n, C.c_int32) for n in ("dtype", "n_pages", "page_size", "max_pages", "n_kv_heads", "head_dim")]
+
+
+class Teacher(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("ids", "values", "lse", "t2d")] + [("n_t2d", C.c_int32), ("k", C.c_int32), ("temperature", C.c_float)]
 
 
 _lib = None
@@ -113,6 +118,19 @@ def lib():
         L.eagle3_paged_attention.argtypes = [C.POINTER(PagedKV), C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_float,
                                              C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.eagle3_paged_attention_workspace.argtypes = [C.POINTER(PagedKV), C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        i32, i64, ptr, f32, size = C.c_int32, C.c_int64, C.c_void_p, C.c_float, C.c_size_t
+        rows = [ptr, i64]                                     # an address and a stride
+        L.eagle3_embed.argtypes = [i32] * 4 + [ptr, ptr, f32, i32] + rows + [ptr]
+        L.eagle3_embed_grad.argtypes = [i32] * 4 + rows + [ptr, f32, i32, i32, ptr, ptr, size, ptr]
+        L.eagle3_embed_grad_workspace.argtypes = [i32] * 3 + [C.POINTER(size)]
+        L.eagle3_add_norm.argtypes = [i32] * 3 + rows + [i32] + rows * 2 + [i32, ptr, f32, i32] + rows + [ptr]
+        L.eagle3_add_norm_codes.argtypes = [i32] * 3 + rows + [i32] + rows * 2 + [i32, ptr, f32, i32] + rows + [ptr, ptr]
+        L.eagle3_add_norm_grad.argtypes = [i32] * 3 + rows + [i32] + rows * 2 + [i32, ptr, f32] + rows + [i32] + rows + [ptr, ptr, size, ptr]
+        L.eagle3_add_norm_grad_workspace.argtypes = [i32] * 2 + [C.POINTER(size)]
+        L.eagle3_distill.argtypes = [i32] * 3 + rows + [C.POINTER(Teacher), ptr, ptr, ptr, size, ptr]
+        L.eagle3_distill_grad.argtypes = [i32] * 3 + rows + [C.POINTER(Teacher), ptr, ptr] + rows + [ptr]
+        L.eagle3_distill_step.argtypes = [i32] * 3 + rows + [C.POINTER(Teacher), ptr, ptr] + rows + [ptr, size, ptr]
+        L.eagle3_distill_workspace.argtypes = [i32] * 2 + [C.POINTER(size)]
         _lib = L
     return _lib
 
@@ -629,3 +647,312 @@ def eagle3_paged_attention(cache, q, kv_len, max_kv_len, scale=None, out=None, w
         d ** -0.5 if scale is None else scale, to, None if lse is None else lse.data_ptr(),
         None if ws is None else ws.data_ptr(), need)
     return (out, lse) if want_lse else out
+
+
+# ---- the ends of a layer stack: embeddings, norms, distillation; calls without a context
+_TYPES = {torch.bfloat16: EAGLE3_BF16, torch.float32: EAGLE3_FP32}
+
+
+def _table(t, gpu, what):
+    """(address, rows, columns, row stride, type) of [rows, columns] in bf16 or fp32, rows any distance apart."""
+    code = _TYPES.get(t.dtype)
+    if code is not None and t.get_device() == gpu and t.dim() == 2:
+        n, d = t.shape
+        s0, s1 = t.stride()
+        if (s1 == 1 or d == 1) and (s0 >= d or n <= 1):
+            return t.data_ptr(), n, d, s0 if n > 1 else d, code
+    _refuse(what, f"bf16 or fp32 rows on cuda:{gpu}, each dense", t)
+
+
+def _like(t, n, d, gpu, what, dtype=None):
+    """_table of a tensor that has to be [n, d], and of this type if one is given."""
+    got = _table(t, gpu, what)
+    if got[1] != n or got[2] != d or (dtype is not None and t.dtype is not dtype):
+        _refuse(what, f"{dtype or 'bf16 or fp32'} [{n}, {d}]", t)
+    return got
+
+
+def _vector(t, d, gpu, what):
+    """(address, type) of a dense [d] in bf16 or fp32."""
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        _refuse(what, "bf16 or fp32", t)
+    return _arg(t, t.dtype, (d,), gpu, what), code
+
+
+def _type(dtype, what):
+    if dtype not in _TYPES:
+        _refuse(what, "torch.bfloat16 or torch.float32", dtype)
+    return _TYPES[dtype]
+
+
+def _even_rows(t):
+    """A gradient as the calls take it: expanded ones and other orders are copied."""
+    return t if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and (t.stride(0) >= t.shape[1] or t.shape[0] <= 1) else t.contiguous()
+
+
+def _workspace(call, sizes, like):
+    """(address, bytes, tensor) of the workspace that a call wants for these sizes."""
+    key = (call, *sizes)
+    need = _workspaces.get(key)
+    if need is None:
+        n = C.c_size_t()
+        _check(getattr(lib(), call)(*sizes, n))
+        if len(_workspaces) >= 256:
+            _workspaces.clear()
+        need = _workspaces[key] = n.value
+    if not need:
+        return None, 0, None
+    t = like.new_empty(need, dtype=torch.uint8)
+    return t.data_ptr(), need, t
+
+
+def _recorded(*tensors):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _not_over_records(out, *inputs):
+    """Results go to new tensors where gradients are recorded."""
+    if out is not None and _recorded(*inputs, *(out if isinstance(out, (tuple, list)) else (out,))):
+        _refuse("out", "None where gradients are recorded", out)
+
+
+def _embed(table, tokens, scale, dtype, out):
+    gpu = _gpu_of(table, "table")
+    tp, V, d, _, code = _table(table, gpu, "table")
+    if not table.is_contiguous() or tokens.dim() != 1:
+        _refuse("table, tokens", "a dense table and int32 [rows]", tokens)
+    rows = tokens.shape[0]
+    tok = _arg(tokens, torch.int32, (rows,), gpu, "tokens")
+    if out is None:
+        out = table.new_empty((rows, d), dtype=table.dtype if dtype is None else dtype)
+    op, _, _, stride, out_code = _like(out, rows, d, gpu, "out", dtype)
+    _on(gpu, lib().eagle3_embed, code, rows, d, V, tp, tok, scale, out_code, op, stride)
+    return out
+
+
+class _Embedded(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, tokens, scale, dtype):
+        ctx.save_for_backward(tokens)
+        ctx.table = table.shape[0], scale, table.dtype
+        return _embed(table, tokens, scale, dtype, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        vocab, scale, dtype = ctx.table
+        return eagle3_embed_grad(_even_rows(dy), ctx.saved_tensors[0], vocab, scale, dtype), None, None, None
+
+
+def eagle3_embed(table, tokens, scale=1.0, dtype=None, out=None):
+    """scale * table[tokens] as [rows, dim] of `dtype` (None: the table's): table [vocab, dim] bf16 or fp32, tokens int32 [rows]; tokens outside the
+    vocabulary give rows of zeros.  `out`: [rows, dim], rows any distance apart.  Recorded for autograd where the table requires a gradient."""
+    if dtype is not None:
+        _type(dtype, "dtype")
+    _not_over_records(out, table)
+    if _recorded(table):
+        return _Embedded.apply(table, tokens, scale, dtype)
+    return _embed(table, tokens, scale, dtype, out)
+
+
+def eagle3_embed_grad(dy, tokens, vocab, scale=1.0, dtype=None, out=None, accumulate=False):
+    """The gradient of eagle3_embed's table, [vocab, dim] of `dtype` (None: that of dy), from that of its result.  `out`: a dense tensor to write it to, or with
+    `accumulate` to add it to.  Nothing is recorded."""
+    gpu = _gpu_of(dy, "dy")
+    dp, rows, d, stride, code = _table(dy, gpu, "dy")
+    tok = _arg(tokens, torch.int32, (rows,), gpu, "tokens")
+    if out is None:
+        if accumulate:
+            _refuse("out", "with accumulate what to add to", out)
+        out = dy.new_empty((vocab, d), dtype=dy.dtype if dtype is None else dtype)
+    op, _, _, _, out_code = _like(out, vocab, d, gpu, "out", dtype)
+    if not out.is_contiguous():
+        _refuse("out", "a dense tensor", out)
+    _not_over_records(out)
+    ws, size, _keep = _workspace("eagle3_embed_grad_workspace", (rows, d, vocab), dy)
+    _on(gpu, lib().eagle3_embed_grad, code, rows, d, vocab, dp, stride, tok, scale, bool(accumulate), out_code, op, ws, size)
+    return out
+
+
+def _norm_inputs(x, gain, residual):
+    """(gpu, rows, d, what every form of the call takes first, but for sum_out): addresses, strides and types."""
+    gpu = _gpu_of(x, "x")
+    xp, n, d, xs, xc = _table(x, gpu, "x")
+    gp, gc = _vector(gain, d, gpu, "gain")
+    if residual is None:
+        return gpu, n, d, (n, d, xc, xp, xs), (xc, None, d), (gc, gp)
+    rp, _, _, rs, rc = _like(residual, n, d, gpu, "residual")
+    if rc != EAGLE3_FP32 and rc != xc:
+        _refuse("residual", f"fp32 or {x.dtype}", residual)
+    return gpu, n, d, (n, d, xc, xp, xs), (rc, rp, rs), (gc, gp)
+
+
+def _sum_out(h, residual, n, d, gpu):
+    """(the sum's tensor, its address, its stride)"""
+    if residual is None:
+        if h is not None:
+            _refuse("out of the sum", "None without residual", h)
+        return None, None, d
+    if h is None:
+        h = torch.empty_like(residual, memory_format=torch.contiguous_format)
+        return h, h.data_ptr(), d
+    hp, _, _, hs, _ = _like(h, n, d, gpu, "out of the sum", residual.dtype)
+    return h, hp, hs
+
+
+def _add_norm(x, gain, eps, residual, dtype, out):
+    gpu, n, d, xa, ra, ga = _norm_inputs(x, gain, residual)
+    y, h = out if isinstance(out, (tuple, list)) else (out, None)
+    h, hp, hs = _sum_out(h, residual, n, d, gpu)
+    if y is None:
+        y = x.new_empty((n, d), dtype=x.dtype if dtype is None else dtype)
+    yp, _, _, ys, yc = _like(y, n, d, gpu, "out", dtype)
+    _on(gpu, lib().eagle3_add_norm, *xa, *ra, hp, hs, *ga, eps, yc, yp, ys)
+    return y if residual is None else (y, h)
+
+
+class _Normed(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gain, eps, residual, dtype):
+        got = _add_norm(x, gain, eps, residual, dtype, None)
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(x if residual is None else got[1], gain)
+        ctx.rest = eps, x.dtype, residual is not None
+        return got
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dh=None):
+        (h, gain), (eps, x_dtype, added) = ctx.saved_tensors, ctx.rest
+        if dy is None:                                        # the sum alone was used, or neither
+            dx, d_sum, d_gain = None if dh is None else dh.to(x_dtype), dh, None
+        else:
+            dx, d_sum, d_gain = _add_norm_grad(_even_rows(dy), h, gain, eps, None if dh is None else _even_rows(dh), x_dtype, ctx.needs_input_grad[1])
+        return dx, d_gain, None, d_sum if added else None, None
+
+
+def eagle3_add_norm(x, gain, eps, residual=None, dtype=None, out=None):
+    """gain * h / sqrt(mean(h^2) + eps) of the rows h = x + residual, [rows, dim] of `dtype` (None: that of x).  x [rows, dim], residual the same in x's type
+    or fp32, gain [dim]; bf16 or fp32, rows any distance apart.  Returns the norm, with residual (norm, h in residual's type).  `out`: the norm's
+    tensor, or (the norm's or None, the sum's or None), which may be x and residual themselves.  Recorded for autograd, which `out` does not allow."""
+    if dtype is not None:
+        _type(dtype, "dtype")
+    _not_over_records(out, x, gain, residual)
+    if _recorded(x, gain, residual):
+        return _Normed.apply(x, gain, eps, residual, dtype)
+    return _add_norm(x, gain, eps, residual, dtype, out)
+
+
+def eagle3_add_norm_codes(x, gain, eps, residual=None, group=0, out=None):
+    """The norm of eagle3_add_norm in 8 bits: (codes float8_e4m3fn [rows, dim], scales fp32 [rows, groups]), with residual (codes, scales, h).  group: columns
+    to a scale, 128, or 0 for one scale a row.  `out`: the sum's tensor.  Nothing is recorded for autograd."""
+    gpu, n, d, xa, ra, ga = _norm_inputs(x, gain, residual)
+    h, hp, hs = _sum_out(out, residual, n, d, gpu)
+    _not_over_records(out, residual)
+    codes = x.new_empty((n, d), dtype=torch.float8_e4m3fn)
+    scales = x.new_empty((n, -(-d // group) if group else 1), dtype=torch.float32)
+    _on(gpu, lib().eagle3_add_norm_codes, *xa, *ra, hp, hs, *ga, eps, group, codes.data_ptr(), d, scales.data_ptr())
+    return (codes, scales) if residual is None else (codes, scales, h)
+
+
+def _add_norm_grad(dy, h, gain, eps, dh, x_dtype, want_gain):
+    gpu = _gpu_of(dy, "dy")
+    yp, n, d, ys, yc = _table(dy, gpu, "dy")
+    hp, _, _, hs, hc = _like(h, n, d, gpu, "h")
+    gp, gc = _vector(gain, d, gpu, "gain")
+    dhp, _, _, dhs, _ = (None, n, d, d, hc) if dh is None else _like(dh, n, d, gpu, "dh", h.dtype)
+    xc = _type(x_dtype, "x_dtype")
+    if hc != EAGLE3_FP32 and hc != xc:
+        _refuse("x_dtype", f"that of h ({h.dtype})", x_dtype)
+    d_sum = torch.empty_like(h, memory_format=torch.contiguous_format)
+    dx = d_sum if xc == hc else h.new_empty((n, d), dtype=x_dtype)
+    d_gain = torch.empty_like(gain) if want_gain else None
+    ws, size, _keep = _workspace("eagle3_add_norm_grad_workspace", (n, d), h) if want_gain else (None, 0, None)
+    _on(gpu, lib().eagle3_add_norm_grad, n, d, yc, yp, ys, hc, hp, hs, dhp, dhs, gc, gp, eps, d_sum.data_ptr(), d, xc, None if dx is d_sum else dx.data_ptr(), d,
+        None if d_gain is None else d_gain.data_ptr(), ws, size)
+    return dx, d_sum, d_gain
+
+
+def eagle3_add_norm_grad(dy, h, gain, eps, dh=None, x_dtype=None):
+    """The gradients of eagle3_add_norm from dy, that of its norm, and dh, that of the sum h where that is used further on: (dx in x_dtype, by default that of dy;
+    d_residual in the type of h, the same tensor if that is the same type; d_gain in that of gain).  Nothing is recorded."""
+    return _add_norm_grad(dy, h, gain, eps, dh, dy.dtype if x_dtype is None else x_dtype, True)
+
+
+def _teacher(logits, ids, values, lse, t2d, temperature):
+    """(gpu, sizes and logits as the calls take them, the teacher's struct)"""
+    gpu = _gpu_of(logits, "logits")
+    xp, n, V, xs, xc = _table(logits, gpu, "logits")
+    if ids.dim() != 2 or values.requires_grad or (lse is not None and lse.requires_grad):
+        _refuse("ids, values, lse", "int32 [rows, k], and fp32 values of which no gradient is wanted", ids)
+    k = ids.shape[1]
+    return gpu, n, V, xs, (xc, n, V, xp, xs), Teacher(
+        _arg(ids, torch.int32, (n, k), gpu, "ids"), _arg(values, torch.float32, (n, k), gpu, "values"), None if lse is None else _arg(lse, torch.float32, (n,), gpu, "lse"),
+        None if t2d is None else _arg(t2d, torch.int32, t2d.shape[:1], gpu, "t2d"), 0 if t2d is None else t2d.shape[0], k, temperature)
+
+
+def _distill(logits, ids, values, lse, t2d, temperature, want_stats):
+    gpu, n, V, _, xa, teacher = _teacher(logits, ids, values, lse, t2d, temperature)
+    loss = logits.new_empty(n, dtype=torch.float32)
+    stats = logits.new_empty((n, 2), dtype=torch.float32) if want_stats else None
+    ws, size, _keep = _workspace("eagle3_distill_workspace", (n, V), logits)
+    _on(gpu, lib().eagle3_distill, *xa, teacher, loss.data_ptr(), None if stats is None else stats.data_ptr(), ws, size)
+    return loss, stats
+
+
+class _Distilled(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, values, lse, t2d, temperature):
+        loss, stats = _distill(logits, ids, values, lse, t2d, temperature, True)
+        ctx.save_for_backward(logits, ids, values, lse, t2d, stats)
+        ctx.temperature = temperature
+        ctx.mark_non_differentiable(stats)
+        return loss, stats
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss, _):
+        logits, ids, values, lse, t2d, stats = ctx.saved_tensors
+        return eagle3_distill_grad(dloss.contiguous(), stats, logits.detach(), ids, values, lse, t2d, ctx.temperature), None, None, None, None, None
+
+
+def eagle3_distill(logits, ids, values, lse=None, t2d=None, temperature=1.0, want_stats=False):
+    """The cross entropy, fp32 [rows], of a student's logits [rows, vocab] (bf16 or fp32, rows any distance apart) against a teacher's logits `values` fp32 [rows, k] of
+    the tokens `ids` int32 [rows, k] (include/eagle3.h: eagle3_teacher): the teacher's probabilities among these tokens, or with lse fp32 [rows] those that it gave
+    them; t2d int32 [n]: the student's ids of the teacher's tokens.  With want_stats (loss, stats fp32 [rows, 2]).  Recorded for autograd."""
+    if _recorded(logits):
+        got = _Distilled.apply(logits, ids, values, lse, t2d, temperature)
+        return got if want_stats else got[0]
+    got = _distill(logits, ids, values, lse, t2d, temperature, want_stats)
+    return got if want_stats else got[0]
+
+
+def _gradient_out(out, logits, n, V, gpu):
+    if out is None:
+        out = logits.new_empty((n, V))
+        return out, out.data_ptr(), V
+    _not_over_records(out)
+    op, _, _, stride, _ = _like(out, n, V, gpu, "out", logits.dtype)
+    return out, op, stride
+
+
+def eagle3_distill_grad(dloss, stats, logits, ids, values, lse=None, t2d=None, temperature=1.0, out=None):
+    """The gradient of eagle3_distill's logits from that of its loss, fp32 [rows], and its stats.  `out`: where to, e.g. the logits themselves.  Nothing is recorded."""
+    gpu, n, V, _, xa, teacher = _teacher(logits, ids, values, lse, t2d, temperature)
+    sp, dp = _arg(stats, torch.float32, (n, 2), gpu, "stats"), _arg(dloss, torch.float32, (n,), gpu, "dloss")
+    out, op, stride = _gradient_out(out, logits, n, V, gpu)
+    _on(gpu, lib().eagle3_distill_grad, *xa, teacher, sp, dp, op, stride)
+    return out
+
+
+def eagle3_distill_step(dloss, logits, ids, values, lse=None, t2d=None, temperature=1.0, out=None):
+    """eagle3_distill and eagle3_distill_grad in one call, where the loss's gradient dloss (fp32 [rows], e.g. a weight for every position) is known before:
+    (loss, d_logits).  `out`: where the gradient goes, e.g. the logits themselves.  Nothing is recorded."""
+    gpu, n, V, _, xa, teacher = _teacher(logits, ids, values, lse, t2d, temperature)
+    dp = _arg(dloss, torch.float32, (n,), gpu, "dloss")
+    loss = logits.new_empty(n, dtype=torch.float32)
+    out, op, stride = _gradient_out(out, logits, n, V, gpu)
+    ws, size, _keep = _workspace("eagle3_distill_workspace", (n, V), logits)
+    _on(gpu, lib().eagle3_distill_step, *xa, teacher, dp, loss.data_ptr(), op, stride, ws, size)
+    return loss, out

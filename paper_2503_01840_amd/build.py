@@ -8,7 +8,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libeagle3.so")
 SOURCES = ["eagle3_api.hip", "gemm_skinny.hip", "gemm_wide.hip", "gemm_f32.hip", "elementwise.hip", "attention.hip", "select.hip",
-           "accept.hip", "commit.hip", "causal_attention.hip", "rotary.hip", "paged.hip", "paged_attention.hip"]
+           "accept.hip", "commit.hip", "causal_attention.hip", "rotary.hip", "paged.hip", "paged_attention.hip",
+           "embed.hip", "norm.hip", "distill.hip"]
 # Kernel arguments, as far as they fit (14 registers), are in registers when a wavefront starts instead of behind its first memory round trip.  That is for
 # arguments of their own, not for members of a struct: what a kernel needs for its first loads comes first in its list.
 FLAGS = ["-O3", "-mllvm", "-amdgpu-kernarg-preload-count=16", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Xclang", "-target-feature", "-Xclang",

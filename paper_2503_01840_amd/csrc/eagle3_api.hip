@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -883,6 +884,172 @@ int eagle3_paged_attention(const eagle3_paged_kv* kv, int32_t B, int32_t n_heads
   const size_t need = paged_attention_workspace(c, kv->dtype, B, n_heads, max_kv_len);
   if (need > workspace_bytes || (need && (!workspace || ((uintptr_t)workspace & 255)))) return EAGLE3_E_STATE;
   CK(launch_paged_attention(c, kv->dtype, B, n_heads, q, q_stride * size, kv_len, max_kv_len, scale, out, lse, workspace, (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+// ---------------------------------------------------------------- embeddings, norms, distillation
+static bool real_type(int32_t t) { return t == EAGLE3_BF16 || t == EAGLE3_FP32; }
+static int64_t size_of(int32_t t) { return t == EAGLE3_FP32 ? 4 : 2; }
+// Rows of n elements of `size` bytes that the kernels can address.
+static bool rows_fit(const void* p, int64_t stride, int64_t n, int64_t size) { return stride >= n && stride < (int64_t)1 << 40 && (uintptr_t)p % size == 0; }
+
+static int workspace_fits(const void* workspace, size_t bytes, size_t need) {
+  return need > bytes || (need && (!workspace || ((uintptr_t)workspace & 255))) ? EAGLE3_E_STATE : EAGLE3_OK;
+}
+
+int eagle3_embed(int32_t dtype, int32_t rows, int32_t dim, int32_t vocab, const void* table, const int32_t* tokens, float scale,
+                 int32_t out_dtype, void* out, int64_t out_stride, eagle3_stream stream) {
+  if (!table || !tokens || !out) return EAGLE3_E_NULL;
+  if (!real_type(dtype) || !real_type(out_dtype)) return EAGLE3_E_SHAPE;
+  if (rows < 1 || rows >= 1 << 24 || dim < 1 || dim > 65536 || vocab < 1) return EAGLE3_E_SHAPE;
+  if (!rows_fit(table, dim, dim, size_of(dtype)) || !rows_fit(out, out_stride, dim, size_of(out_dtype))) return EAGLE3_E_SHAPE;
+  CK(launch_embed({tokens, table, rows, dim, vocab, scale, out, out_stride}, dtype == EAGLE3_BF16, out_dtype == EAGLE3_BF16, (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+static int embed_grad_sizes(int32_t rows, int32_t dim, int32_t vocab) {
+  if (rows < 1 || rows >= 1 << 22 || dim < 1 || dim > 65536 || (int64_t)rows * dim >= (int64_t)1 << 36 || vocab < 1 || vocab >= 1 << 27) return EAGLE3_E_SHAPE;
+  return EAGLE3_OK;
+}
+
+int eagle3_embed_grad_workspace(int32_t rows, int32_t dim, int32_t vocab, size_t* bytes) {
+  if (!bytes) return EAGLE3_E_NULL;
+  TRY(embed_grad_sizes(rows, dim, vocab));
+  *bytes = embed_grad_workspace(rows, dim);
+  return EAGLE3_OK;
+}
+
+int eagle3_embed_grad(int32_t dtype, int32_t rows, int32_t dim, int32_t vocab, const void* dy, int64_t dy_stride, const int32_t* tokens, float scale,
+                      int32_t accumulate, int32_t out_dtype, void* d_table, void* workspace, size_t workspace_bytes, eagle3_stream stream) {
+  if (!dy || !tokens || !d_table) return EAGLE3_E_NULL;
+  if (!real_type(dtype) || !real_type(out_dtype)) return EAGLE3_E_SHAPE;
+  TRY(embed_grad_sizes(rows, dim, vocab));
+  if (!rows_fit(dy, dy_stride, dim, size_of(dtype)) || !rows_fit(d_table, dim, dim, size_of(out_dtype))) return EAGLE3_E_SHAPE;
+  TRY(workspace_fits(workspace, workspace_bytes, embed_grad_workspace(rows, dim)));
+  CK(launch_embed_grad({tokens, dy, dy_stride, rows, dim, vocab, scale, d_table, nullptr}, dtype == EAGLE3_BF16, out_dtype == EAGLE3_BF16, accumulate != 0,
+                       workspace, (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+static int norm_sizes(int32_t rows, int32_t dim) { return rows < 1 || rows >= 1 << 24 || dim < 1 || dim > 16384 ? EAGLE3_E_SHAPE : EAGLE3_OK; }
+
+// What both forms of the norm want; the output apart.
+static int norm_rows(const NormRows& a, int32_t x_dtype, int32_t sum_dtype, int32_t gain_dtype) {
+  if (!a.x || !a.gain || !a.out || (a.residual != nullptr) != (a.sum_out != nullptr)) return EAGLE3_E_NULL;
+  if (!real_type(x_dtype) || !real_type(gain_dtype)) return EAGLE3_E_SHAPE;
+  TRY(norm_sizes(a.rows, a.dim));
+  if (!(a.eps >= 0.f) || !rows_fit(a.x, a.x_stride, a.dim, size_of(x_dtype)) || !rows_fit(a.gain, a.dim, a.dim, size_of(gain_dtype))) return EAGLE3_E_SHAPE;
+  if (!a.residual) return EAGLE3_OK;
+  if (sum_dtype != EAGLE3_FP32 && sum_dtype != x_dtype) return EAGLE3_E_SHAPE;
+  if (!rows_fit(a.residual, a.residual_stride, a.dim, size_of(sum_dtype)) || !rows_fit(a.sum_out, a.sum_stride, a.dim, size_of(sum_dtype))) return EAGLE3_E_SHAPE;
+  return a.sum_out == a.residual && a.sum_stride != a.residual_stride ? EAGLE3_E_SHAPE : EAGLE3_OK;
+}
+static int norm_type(int32_t dtype) { return dtype == EAGLE3_BF16 ? NORM_BF16 : NORM_FP32; }
+
+int eagle3_add_norm(int32_t rows, int32_t dim, int32_t x_dtype, const void* x, int64_t x_stride, int32_t sum_dtype, const void* residual,
+                    int64_t residual_stride, void* sum_out, int64_t sum_stride, int32_t gain_dtype, const void* gain, float eps, int32_t out_dtype,
+                    void* out, int64_t out_stride, eagle3_stream stream) {
+  const NormRows a = {x, residual, sum_out, gain, out, nullptr, x_stride, residual_stride, sum_stride, out_stride, rows, dim, 0, gain_dtype == EAGLE3_BF16, eps};
+  TRY(norm_rows(a, x_dtype, sum_dtype, gain_dtype));
+  if (!real_type(out_dtype) || !rows_fit(out, out_stride, dim, size_of(out_dtype))) return EAGLE3_E_SHAPE;
+  if (out == x && (out_dtype != x_dtype || out_stride != x_stride)) return EAGLE3_E_SHAPE;
+  CK(launch_norm_rows(a, norm_type(x_dtype), norm_type(residual ? sum_dtype : x_dtype), norm_type(out_dtype), (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+int eagle3_add_norm_codes(int32_t rows, int32_t dim, int32_t x_dtype, const void* x, int64_t x_stride, int32_t sum_dtype, const void* residual,
+                          int64_t residual_stride, void* sum_out, int64_t sum_stride, int32_t gain_dtype, const void* gain, float eps, int32_t group,
+                          uint8_t* codes, int64_t codes_stride, float* scales, eagle3_stream stream) {
+  const NormRows a = {x, residual, sum_out, gain, codes, scales, x_stride, residual_stride, sum_stride, codes_stride, rows, dim, group, gain_dtype == EAGLE3_BF16, eps};
+  if (!scales) return EAGLE3_E_NULL;
+  TRY(norm_rows(a, x_dtype, sum_dtype, gain_dtype));
+  if ((group != 0 && group != 128) || !rows_fit(codes, codes_stride, dim, 1) || (uintptr_t)scales % 4) return EAGLE3_E_SHAPE;
+  CK(launch_norm_rows(a, norm_type(x_dtype), norm_type(residual ? sum_dtype : x_dtype), NORM_CODES, (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+int eagle3_add_norm_grad_workspace(int32_t rows, int32_t dim, size_t* bytes) {
+  if (!bytes) return EAGLE3_E_NULL;
+  TRY(norm_sizes(rows, dim));
+  *bytes = norm_grad_workspace(rows, dim);
+  return EAGLE3_OK;
+}
+
+int eagle3_add_norm_grad(int32_t rows, int32_t dim, int32_t dy_dtype, const void* dy, int64_t dy_stride, int32_t sum_dtype, const void* h,
+                         int64_t h_stride, const void* dh, int64_t dh_stride, int32_t gain_dtype, const void* gain, float eps, void* d_sum,
+                         int64_t d_sum_stride, int32_t x_dtype, void* dx, int64_t dx_stride, void* d_gain, void* workspace, size_t workspace_bytes,
+                         eagle3_stream stream) {
+  if (!dy || !h || !gain || (!d_sum && !dx)) return EAGLE3_E_NULL;
+  if (!real_type(dy_dtype) || !real_type(sum_dtype) || !real_type(gain_dtype) || !real_type(x_dtype)) return EAGLE3_E_SHAPE;
+  if (sum_dtype != EAGLE3_FP32 && sum_dtype != x_dtype) return EAGLE3_E_SHAPE;
+  TRY(norm_sizes(rows, dim));
+  const int64_t s = size_of(sum_dtype);
+  if (!(eps >= 0.f) || !rows_fit(gain, dim, dim, size_of(gain_dtype)) || !rows_fit(dy, dy_stride, dim, size_of(dy_dtype)) || !rows_fit(h, h_stride, dim, s)) return EAGLE3_E_SHAPE;
+  if ((dh && !rows_fit(dh, dh_stride, dim, s)) || (d_sum && !rows_fit(d_sum, d_sum_stride, dim, s)) || (dx && !rows_fit(dx, dx_stride, dim, size_of(x_dtype)))) return EAGLE3_E_SHAPE;
+  if ((dh && d_sum == dh && d_sum_stride != dh_stride) || (uintptr_t)d_gain % size_of(gain_dtype)) return EAGLE3_E_SHAPE;
+  if (d_gain) TRY(workspace_fits(workspace, workspace_bytes, norm_grad_workspace(rows, dim)));
+  const NormRows a = {nullptr, nullptr, nullptr, gain, nullptr, nullptr, 0, 0, 0, 0, rows, dim, 0, gain_dtype == EAGLE3_BF16, eps};
+  CK(launch_norm_rows_grad({a, dy, h, dh, d_sum, dx, d_gain, d_gain ? (float*)workspace : nullptr, dy_stride, h_stride, dh_stride, d_sum_stride, dx_stride},
+                           norm_type(dy_dtype), norm_type(sum_dtype), norm_type(x_dtype), (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+static int distill_sizes(int32_t rows, int32_t vocab) { return rows < 1 || rows >= 1 << 24 || vocab < 1 || vocab >= 1 << 27 ? EAGLE3_E_SHAPE : EAGLE3_OK; }
+
+static int distill_rows(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t stride, const eagle3_teacher* t, DistillRows& a) {
+  if (!logits || !t || !t->ids || !t->values) return EAGLE3_E_NULL;
+  if (!real_type(dtype) || t->k < 1 || t->k > 1024 || (t->t2d && t->n_t2d < 1) || !(t->temperature > 0.f) || !std::isfinite(t->temperature)) return EAGLE3_E_SHAPE;
+  TRY(distill_sizes(rows, vocab));
+  if (!rows_fit(logits, stride, vocab, size_of(dtype))) return EAGLE3_E_SHAPE;
+  a = {logits, stride, rows, vocab, t->ids, t->values, t->lse, t->t2d, t->n_t2d, t->k, t->temperature, nullptr, nullptr, nullptr, nullptr, 0};
+  return EAGLE3_OK;
+}
+
+int eagle3_distill_workspace(int32_t rows, int32_t vocab, size_t* bytes) {
+  if (!bytes) return EAGLE3_E_NULL;
+  TRY(distill_sizes(rows, vocab));
+  *bytes = distill_workspace(rows, vocab);
+  return EAGLE3_OK;
+}
+
+int eagle3_distill(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t logits_stride, const eagle3_teacher* teacher, float* loss,
+                   float* stats, void* workspace, size_t workspace_bytes, eagle3_stream stream) {
+  DistillRows a;
+  if (!loss) return EAGLE3_E_NULL;
+  TRY(distill_rows(dtype, rows, vocab, logits, logits_stride, teacher, a));
+  if ((uintptr_t)stats % 8) return EAGLE3_E_SHAPE;
+  TRY(workspace_fits(workspace, workspace_bytes, distill_workspace(rows, vocab)));
+  a.loss = loss, a.stats = stats;
+  CK(launch_distill(a, dtype == EAGLE3_BF16, workspace, (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+// Where a gradient goes: apart from the logits, or exactly over them.
+static bool gradient_fits(const void* d_logits, int64_t d_stride, const DistillRows& a, int32_t dtype) {
+  return rows_fit(d_logits, d_stride, a.vocab, size_of(dtype)) && (d_logits != a.logits || d_stride == a.stride);
+}
+
+int eagle3_distill_grad(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t logits_stride, const eagle3_teacher* teacher,
+                        const float* stats, const float* dloss, void* d_logits, int64_t d_logits_stride, eagle3_stream stream) {
+  DistillRows a;
+  if (!stats || !dloss || !d_logits) return EAGLE3_E_NULL;
+  TRY(distill_rows(dtype, rows, vocab, logits, logits_stride, teacher, a));
+  if ((uintptr_t)stats % 8 || !gradient_fits(d_logits, d_logits_stride, a, dtype)) return EAGLE3_E_SHAPE;
+  a.stats = (float*)stats, a.dloss = dloss, a.d_logits = d_logits, a.d_stride = d_logits_stride;
+  CK(launch_distill_grad(a, dtype == EAGLE3_BF16, (hipStream_t)stream));
+  return EAGLE3_OK;
+}
+
+int eagle3_distill_step(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t logits_stride, const eagle3_teacher* teacher,
+                        const float* dloss, float* loss, void* d_logits, int64_t d_logits_stride, void* workspace, size_t workspace_bytes,
+                        eagle3_stream stream) {
+  DistillRows a;
+  if (!loss || !dloss || !d_logits) return EAGLE3_E_NULL;
+  TRY(distill_rows(dtype, rows, vocab, logits, logits_stride, teacher, a));
+  if (!gradient_fits(d_logits, d_logits_stride, a, dtype)) return EAGLE3_E_SHAPE;
+  TRY(workspace_fits(workspace, workspace_bytes, distill_workspace(rows, vocab)));
+  a.loss = loss, a.dloss = dloss, a.d_logits = d_logits, a.d_stride = d_logits_stride;
+  CK(launch_distill_step(a, dtype == EAGLE3_BF16, workspace, (hipStream_t)stream));
   return EAGLE3_OK;
 }
 

@@ -1,0 +1,427 @@
+// Rows of an embedding table, and the table's gradient.
+//
+// Rows: a wavefront takes a row or a part of it, the token once for all its lanes, 16 bytes to a lane and load.  Bound by bytes.
+//
+// Gradient: the rows' tokens are sorted first (stable, digits of at most 9 bits), so that a token's rows are neighbours and their sum has an order of its own.
+// Then CHUNK sorted places at a time are summed by a wavefront for 64 N columns each; a token's sum that lies within them is written at once, the
+// ends of one that does not go to the workspace and are added by the next launch.  Other wavefronts of the same launch fill the table's other rows with zeros.
+// Bound by bytes: the rows read, the table written once.
+#include <algorithm>
+
+#include "elements.hpp"
+#include "kernels.hpp"
+
+namespace {
+
+// ---------------------------------------------------------------- rows
+template <typename T, typename O, int N>
+__global__ __launch_bounds__(256) void embed_kernel(const int32_t* tokens, const T* table, int rows, int dim, int vocab, float scale, O* out, long long stride, int share) {
+  constexpr int U = N == 1 ? 8 : 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = blockIdx.x * 4 + wave;
+  if (r >= rows) return;
+  const int token = tokens[r], pieces = dim / N, first = blockIdx.y * share, last = min(pieces, first + share);
+  const bool seen = token >= 0 && token < vocab;
+  const T* from = table + (size_t)(seen ? token : 0) * dim;
+  O* to = out + (size_t)r * stride;
+  for (int p0 = first; p0 < last; p0 += 64 * U) {
+    Elems<T, N> e[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int p = p0 + 64 * j + lane;
+      if (seen && p < last) e[j].load(from + (size_t)p * N);
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int p = p0 + 64 * j + lane;
+      if (p < last) {
+        float f[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = seen ? scale * e[j].at(i) : 0.f;
+        store_elems<N>(to + (size_t)p * N, f);
+      }
+    }
+  }
+}
+
+template <typename T, typename O, int N>
+hipError_t rows_of(const EmbedRows& a, hipStream_t st) {
+  constexpr int U = N == 1 ? 8 : 4;
+  const int most = (a.dim / N + 63) / 64, want = std::max(1, std::min(most, 8192 / a.rows));     // few rows: each over several wavefronts
+  const int each = (most + want - 1) / want, share = 64 * (each > U ? (each + U - 1) / U * U : each);
+  const dim3 grid((a.rows + 3) / 4, (a.dim / N + share - 1) / share);
+  hipLaunchKernelGGL((embed_kernel<T, O, N>), grid, dim3(256), 0, st, a.tokens, (const T*)a.table, a.rows, a.dim, a.vocab, a.scale, (O*)a.out, a.stride, share);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- tokens in order
+// A tile of 4096 places to a workgroup of 16 wavefronts: wavefront w has places 256 w + 64 r + lane, r < 4, so that the order of places is that of (w, r, lane).
+constexpr int TILE = 4096, DIGITS = 512;
+
+__device__ __forceinline__ uint32_t key_of(const int32_t* tokens, int i, int n, int vocab) {
+  if (i >= n) return 0xFFFFFFFFu;                             // behind everything
+  const int t = tokens[i];
+  return t >= 0 && t < vocab ? (uint32_t)t : (uint32_t)vocab; // padding behind the vocabulary
+}
+
+// The place that each of a tile's keys takes by one digit, in order among equal ones: from base[digit] on (ONE: from the tile's own counts).
+template <bool ONE>
+__device__ __forceinline__ void ranks(const uint32_t* key, int shift, int bits, uint16_t (*count)[DIGITS], uint32_t* base, uint32_t* wave_sums, int* to) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const uint32_t mask = (1u << bits) - 1;
+  for (int i = threadIdx.x; i < 16 * DIGITS; i += 1024) count[i / DIGITS][i % DIGITS] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const uint32_t d = (key[r] >> shift) & mask;
+    uint64_t same = ~0ull;
+    for (int b = 0; b < bits; ++b) {
+      const bool one = (d >> b) & 1;
+      const uint64_t vote = __ballot(one);
+      same &= one ? vote : ~vote;
+    }
+    const int before = __popcll(same & ((1ull << lane) - 1)), so_far = count[wave][d];
+    to[r] = so_far + before;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // every lane has read its count
+    __builtin_amdgcn_wave_barrier();
+    if (before == 0) count[wave][d] = (uint16_t)(so_far + __popcll(same));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  // counts of the wavefronts before; the tile's count of a digit
+  uint32_t total = 0;
+  if (threadIdx.x < DIGITS) {
+    for (int w = 0; w < 16; ++w) {
+      const uint32_t c = count[w][threadIdx.x];
+      count[w][threadIdx.x] = (uint16_t)total;
+      total += c;
+    }
+  }
+  if constexpr (ONE) {                                        // base = sums of the digits below
+    uint32_t sum = total;
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t v = __shfl_up(sum, o, 64);
+      if (lane >= o) sum += v;
+    }
+    if (lane == 63 && wave < DIGITS / 64) wave_sums[wave] = sum;
+    __syncthreads();
+    if (threadIdx.x < DIGITS) {
+      for (int w = 0; w < wave; ++w) sum += wave_sums[w];
+      base[threadIdx.x] = sum - total;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const uint32_t d = (key[r] >> shift) & mask;
+    to[r] += base[d] + count[wave][d];
+  }
+}
+
+// All of at most TILE places, in one workgroup.
+__global__ __launch_bounds__(1024) void sort_tile_kernel(const int32_t* tokens, int n, int vocab, int passes, int bits, int32_t* token_out, int32_t* row_out) {
+  __shared__ uint16_t count[16][DIGITS];
+  __shared__ uint32_t base[DIGITS], wave_sums[DIGITS / 64];
+  __shared__ uint32_t keys[TILE];
+  __shared__ uint16_t rows[TILE];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  uint32_t key[4];
+  int row[4], to[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    row[r] = 256 * wave + 64 * r + lane;
+    key[r] = key_of(tokens, row[r], n, vocab);
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+    ranks<true>(key, pass * bits, bits, count, base, wave_sums, to);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      keys[to[r]] = key[r];
+      rows[to[r]] = (uint16_t)row[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = 256 * wave + 64 * r + lane;
+      key[r] = keys[i];
+      row[r] = rows[i];
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int i = 256 * wave + 64 * r + lane;
+    if (i < n) {
+      token_out[i] = (int32_t)key[r];
+      row_out[i] = row[r];
+    }
+  }
+}
+
+// One digit of more places: a tile's counts, then each tile's places.
+__global__ __launch_bounds__(1024) void sort_count_kernel(const int32_t* tokens, int n, int vocab, int shift, int bits, uint32_t* hist) {
+  __shared__ uint32_t count[DIGITS];
+  if (threadIdx.x < DIGITS) count[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int i = blockIdx.x * TILE + r * 1024 + threadIdx.x;
+    if (i < n) atomicAdd(&count[(key_of(tokens, i, n, vocab) >> shift) & ((1u << bits) - 1)], 1u);
+  }
+  __syncthreads();
+  if (threadIdx.x < DIGITS) hist[(size_t)blockIdx.x * DIGITS + threadIdx.x] = count[threadIdx.x];
+}
+__global__ __launch_bounds__(1024) void sort_place_kernel(const int32_t* tokens, const int32_t* rows, int n, int vocab, int shift, int bits, const uint32_t* hist, int tiles,
+                                                          int32_t* token_out, int32_t* row_out) {
+  __shared__ uint16_t count[16][DIGITS];
+  __shared__ uint32_t base[DIGITS], wave_sums[DIGITS / 64];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  uint32_t key[4];
+  int row[4], to[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int i = blockIdx.x * TILE + 256 * wave + 64 * r + lane;
+    key[r] = key_of(tokens, i, n, vocab);
+    row[r] = i < n && rows ? rows[i] : i;
+  }
+  // base = the count of smaller digits in all tiles, and of this one in the tiles before
+  uint32_t all = 0, before = 0;
+  if (threadIdx.x < DIGITS) {
+    const uint32_t* h = hist + threadIdx.x;
+#pragma unroll 8
+    for (int t = 0; t < tiles; ++t) {
+      const uint32_t c = h[(size_t)t * DIGITS];
+      all += c;
+      before += t < (int)blockIdx.x ? c : 0;
+    }
+  }
+  uint32_t sum = all;
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t v = __shfl_up(sum, o, 64);
+    if (lane >= o) sum += v;
+  }
+  if (lane == 63 && wave < DIGITS / 64) wave_sums[wave] = sum;
+  __syncthreads();
+  if (threadIdx.x < DIGITS) {
+    for (int w = 0; w < wave; ++w) sum += wave_sums[w];
+    base[threadIdx.x] = sum - all + before;
+  }
+  ranks<false>(key, shift, bits, count, base, wave_sums, to);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int i = blockIdx.x * TILE + 256 * wave + 64 * r + lane;
+    if (i < n) {                                              // those behind the end have the largest digit and are its last ones
+      token_out[to[r]] = (int32_t)key[r];
+      row_out[to[r]] = row[r];
+    }
+  }
+}
+
+// ---------------------------------------------------------------- sums
+constexpr int CHUNK = 32, BATCH = 8, EMPTY_ROWS = 16;
+
+// Wavefronts below `sums` sum a chunk's rows for 64 N columns; the others look for tokens that do not occur among EMPTY_ROWS of the table and write zeros.
+// partial: [chunk][2][dim]: sums of a chunk's first token that began before it, and of its last one that goes on behind it.
+template <typename T, typename O, int N, bool ADD>
+__global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restrict__ token, const int32_t* __restrict__ row_of, int n, int dim, int vocab, EmbedGrad g, int slabs, int sums) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int task = blockIdx.x * 4 + wave, pieces = dim / N;
+  O* table = (O*)g.d_table;
+  if (task >= sums) {
+    if (ADD) return;                                          // the rest of the last workgroup
+    const long long v0 = (long long)(task - sums) * EMPTY_ROWS;
+    if (v0 >= vocab) return;
+    // lanes 0..15: does token v0 + lane occur?
+    const int v = (int)min((long long)vocab, v0 + (lane & (EMPTY_ROWS - 1)));
+    int lo = 0, hi = n;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (token[mid] < v) lo = mid + 1;
+      else hi = mid;
+    }
+    const bool absent = v < vocab && !(lo < n && token[lo] == v);
+    const uint64_t empty = __ballot(absent);
+    float zeros[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) zeros[i] = 0.f;
+    for (int i = 0; i < EMPTY_ROWS; ++i) {
+      if (!(empty >> i & 1)) continue;
+      O* to = table + (size_t)(v0 + i) * dim;
+      for (int p = lane; p < pieces; p += 64) store_elems<N>(to + (size_t)p * N, zeros);
+    }
+    return;
+  }
+  const int chunk = task / slabs, p = (task - chunk * slabs) * 64 + lane, first = chunk * CHUNK, last = min(n, first + CHUNK);
+  const bool has = p < pieces;
+  int current = token[first];
+  if (current >= vocab) return;                               // padding only
+  bool began_before = first > 0 && token[first - 1] == current;
+  const T* dy = (const T*)g.dy + (size_t)p * N;
+  float sum[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum[i] = 0.f;
+  // what is left of `current` goes to the table, or to the workspace
+  auto leave = [&](bool goes_on) {
+    if (!has) return;
+    if (began_before || goes_on) {
+      float* to = g.partial + ((size_t)chunk * 2 + (began_before ? 0 : 1)) * dim + (size_t)p * N;
+      store_elems<N>(to, sum);
+      return;
+    }
+    O* to = table + (size_t)current * dim + (size_t)p * N;
+    float f[N];
+    if constexpr (ADD) {
+      Elems<O, N> old;
+      old.load(to);
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[i] = fmaf(g.scale, sum[i], old.at(i));
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) f[i] = g.scale * sum[i];
+    }
+    store_elems<N>(to, f);
+  };
+  for (int at = first; at < last; at += BATCH) {
+    Elems<T, N> e[BATCH];
+    int tok[BATCH];
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      tok[j] = at + j < last ? token[at + j] : vocab;
+      if (tok[j] < vocab && has) e[j].load(dy + (size_t)row_of[at + j] * g.stride);
+    }
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      if (at + j >= last) break;
+      if (tok[j] != current) {
+        leave(false);
+        current = tok[j];
+        began_before = false;
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] = 0.f;
+      }
+      if (current >= vocab) return;
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] += has ? e[j].at(i) : 0.f;
+    }
+  }
+  leave(last < n && token[last] == current);
+}
+
+// Tokens whose rows lie in several chunks: workgroup (chunk, 64 N columns) adds the parts of the one that begins in this chunk and goes on behind it, a quarter of
+// them to each wavefront.
+template <typename O, int N, bool ADD>
+__global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restrict__ token, int n, int dim, int vocab, EmbedGrad g) {
+  __shared__ float part[4][64 * N];
+  const int chunk = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, p = blockIdx.y * 64 + lane;
+  const int first = chunk * CHUNK, end = first + CHUNK;
+  if (end >= n) return;
+  const int v = token[end - 1];
+  if (v >= vocab || token[end] != v || (token[first] == v && first > 0 && token[first - 1] == v)) return;
+  int lo = end, hi = n;                                       // behind its last row
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (token[mid] <= v) lo = mid + 1;
+    else hi = mid;
+  }
+  const int parts = (lo - 1) / CHUNK - chunk + 1, share = (parts + 3) / 4;
+  const bool has = p < dim / N;
+  float sum[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum[i] = 0.f;
+  if (has) {
+#pragma unroll 4
+    for (int c = wave * share; c < min(parts, (wave + 1) * share); ++c) {
+      Elems<float, N> e;
+      e.load(g.partial + ((size_t)(chunk + c) * 2 + (c ? 0 : 1)) * dim + (size_t)p * N);
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] += e.at(i);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) part[wave][lane * N + i] = sum[i];
+  __syncthreads();
+  if (wave || !has) return;
+  float f[N];
+  O* to = (O*)g.d_table + (size_t)v * dim + (size_t)p * N;
+  Elems<O, N> old;
+  if constexpr (ADD) old.load(to);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float s = (part[0][lane * N + i] + part[1][lane * N + i]) + (part[2][lane * N + i] + part[3][lane * N + i]);
+    f[i] = ADD ? fmaf(g.scale, s, old.at(i)) : g.scale * s;
+  }
+  store_elems<N>(to, f);
+}
+
+// ---------------------------------------------------------------- the workspace: keys and rows, twice, counts, parts
+size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
+int chunks_of(int rows) { return (rows + CHUNK - 1) / CHUNK; }
+
+// Sorted tokens and their rows, in *token and *row.
+hipError_t sort_tokens(const EmbedGrad& g, char* ws, const int32_t** token, const int32_t** row, hipStream_t st) {
+  const int n = g.rows;
+  int bits = 1;                                               // of the largest key, the vocabulary's size
+  while (bits < 31 && g.vocab >> bits) ++bits;
+  const int passes = (bits + 8) / 9, each = (bits + passes - 1) / passes;
+  const size_t array = aligned((size_t)n * sizeof(int32_t));
+  int32_t* key[2] = {(int32_t*)ws, (int32_t*)(ws + array)};
+  int32_t* rows[2] = {(int32_t*)(ws + 2 * array), (int32_t*)(ws + 3 * array)};
+  if (n <= TILE) {
+    hipLaunchKernelGGL(sort_tile_kernel, dim3(1), dim3(1024), 0, st, g.tokens, n, g.vocab, passes, each, key[0], rows[0]);
+    *token = key[0], *row = rows[0];
+    return hipGetLastError();
+  }
+  uint32_t* hist = (uint32_t*)(ws + 4 * array);
+  const int tiles = (n + TILE - 1) / TILE;
+  const int32_t* from = g.tokens;
+  const int32_t* from_rows = nullptr;
+  for (int pass = 0; pass < passes; ++pass) {
+    hipLaunchKernelGGL(sort_count_kernel, dim3(tiles), dim3(1024), 0, st, from, n, g.vocab, pass * each, each, hist);
+    hipLaunchKernelGGL(sort_place_kernel, dim3(tiles), dim3(1024), 0, st, from, from_rows, n, g.vocab, pass * each, each, hist, tiles, key[pass & 1], rows[pass & 1]);
+    from = key[pass & 1], from_rows = rows[pass & 1];
+  }
+  *token = from, *row = from_rows;
+  return hipGetLastError();
+}
+
+template <typename T, typename O, int N, bool ADD>
+hipError_t sums_of(EmbedGrad g, char* ws, hipStream_t st) {
+  const int32_t *token, *row;
+  hipError_t e = sort_tokens(g, ws, &token, &row, st);
+  if (e != hipSuccess) return e;
+  g.partial = (float*)(ws + 4 * aligned((size_t)g.rows * sizeof(int32_t)) + aligned((size_t)((g.rows + TILE - 1) / TILE) * DIGITS * sizeof(uint32_t)));
+  const int slabs = (g.dim / N + 63) / 64, sums = chunks_of(g.rows) * slabs, empty = ADD ? 0 : (g.vocab + EMPTY_ROWS - 1) / EMPTY_ROWS;
+  hipLaunchKernelGGL((embed_sum_kernel<T, O, N, ADD>), dim3((unsigned)(((long long)sums + empty + 3) / 4)), dim3(256), 0, st, token, row, g.rows, g.dim, g.vocab, g, slabs, sums);
+  e = hipGetLastError();
+  if (e != hipSuccess || g.rows <= CHUNK) return e;
+  hipLaunchKernelGGL((embed_join_kernel<O, N, ADD>), dim3(chunks_of(g.rows), slabs), dim3(256), 0, st, token, g.rows, g.dim, g.vocab, g);
+  return hipGetLastError();
+}
+
+template <typename T, typename O>
+hipError_t sums_as(const EmbedGrad& g, bool add, char* ws, hipStream_t st) {
+  const bool wide = g.dim % 8 == 0 && rows_at_16(g.dy, g.stride, sizeof(T)) && rows_at_16(g.d_table, g.dim, sizeof(O));
+  if (wide) return add ? sums_of<T, O, 8, true>(g, ws, st) : sums_of<T, O, 8, false>(g, ws, st);
+  return add ? sums_of<T, O, 1, true>(g, ws, st) : sums_of<T, O, 1, false>(g, ws, st);
+}
+
+template <typename T, typename O> hipError_t rows_as(const EmbedRows& a, hipStream_t st) {
+  const bool wide = a.dim % 8 == 0 && rows_at_16(a.table, a.dim, sizeof(T)) && rows_at_16(a.out, a.stride, sizeof(O));
+  return wide ? rows_of<T, O, 8>(a, st) : rows_of<T, O, 1>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_embed(const EmbedRows& a, bool table_bf16, bool out_bf16, hipStream_t st) {
+  if (table_bf16) return out_bf16 ? rows_as<bf16_t, bf16_t>(a, st) : rows_as<bf16_t, float>(a, st);
+  return out_bf16 ? rows_as<float, bf16_t>(a, st) : rows_as<float, float>(a, st);
+}
+
+size_t embed_grad_workspace(int rows, int dim) {
+  return 4 * aligned((size_t)rows * sizeof(int32_t)) + aligned((size_t)((rows + TILE - 1) / TILE) * DIGITS * sizeof(uint32_t)) +
+         (rows > CHUNK ? aligned((size_t)chunks_of(rows) * 2 * dim * sizeof(float)) : 0);
+}
+
+hipError_t launch_embed_grad(const EmbedGrad& g, bool dy_bf16, bool out_bf16, bool add, void* ws, hipStream_t st) {
+  if (dy_bf16) return out_bf16 ? sums_as<bf16_t, bf16_t>(g, add, (char*)ws, st) : sums_as<bf16_t, float>(g, add, (char*)ws, st);
+  return out_bf16 ? sums_as<float, bf16_t>(g, add, (char*)ws, st) : sums_as<float, float>(g, add, (char*)ws, st);
+}

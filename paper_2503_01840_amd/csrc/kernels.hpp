@@ -240,3 +240,77 @@ hipError_t launch_paged_rows(const PagedView& c, int dtype, bool read, int B, in
 size_t paged_attention_workspace(const PagedView& c, int dtype, int B, int H, int max_len);
 hipError_t launch_paged_attention(const PagedView& c, int dtype, int B, int H, const void* q, long long q_bytes, const int32_t* kv_len, int max_len,
                                   float scale, void* out, float* lse, void* workspace, hipStream_t st);
+
+// ---------------------------------------------------------------- embeddings (embed.hip)
+struct EmbedRows {
+  const int32_t* tokens;
+  const void* table;        // [vocab, dim]
+  int rows, dim, vocab;
+  float scale;
+  void* out;
+  long long stride;
+};
+hipError_t launch_embed(const EmbedRows& a, bool table_bf16, bool out_bf16, hipStream_t st);
+struct EmbedGrad {
+  const int32_t* tokens;
+  const void* dy;
+  long long stride;
+  int rows, dim, vocab;
+  float scale;
+  void* d_table;
+  float* partial;           // the kernels' own
+};
+size_t embed_grad_workspace(int rows, int dim);
+hipError_t launch_embed_grad(const EmbedGrad& g, bool dy_bf16, bool out_bf16, bool add, void* ws, hipStream_t st);
+
+// ---------------------------------------------------------------- norms (norm.hip)
+enum { NORM_FP32 = 0, NORM_BF16 = 1, NORM_CODES = 2 };
+#define NORM_GRAD_PARTS 512 /* workgroups of a gradient at most: that many sums of each gain's gradient */
+struct NormRows {
+  const void* x;
+  const void* residual;     // null: h = x
+  void* sum_out;
+  const void* gain;
+  void* out;
+  float* scales;            // codes
+  long long x_stride, residual_stride, sum_stride, out_stride;
+  int rows, dim, group;
+  bool gain_bf16;
+  float eps;
+};
+hipError_t launch_norm_rows(const NormRows& a, int x_type, int sum_type, int out_type, hipStream_t st);
+struct NormGradRows {
+  NormRows fwd;             // rows, dim, gain, eps
+  const void* dy;
+  const void* h;
+  const void* dh;           // may be null, like every output
+  void* d_sum;
+  void* dx;
+  void* d_gain;
+  float* partial;           // [NORM_GRAD_PARTS, dim] with d_gain
+  long long dy_stride, h_stride, dh_stride, d_sum_stride, dx_stride;
+};
+size_t norm_grad_workspace(int rows, int dim);
+hipError_t launch_norm_rows_grad(const NormGradRows& b, int dy_type, int sum_type, int x_type, hipStream_t st);
+
+// ---------------------------------------------------------------- distillation (distill.hip)
+struct DistillRows {
+  const void* logits;
+  long long stride;
+  int rows, vocab;
+  const int32_t* ids;       // the teacher: include/eagle3.h
+  const float* values;
+  const float* lse;
+  const int32_t* t2d;
+  int n_t2d, k;
+  float temperature;
+  const float* dloss;
+  float* loss;
+  float* stats;             // [rows, 2]
+  void* d_logits;
+  long long d_stride;
+};
+size_t distill_workspace(int rows, int vocab);
+hipError_t launch_distill(const DistillRows& a, bool bf16, void* ws, hipStream_t st);
+hipError_t launch_distill_grad(const DistillRows& a, bool bf16, hipStream_t st);
+hipError_t launch_distill_step(const DistillRows& a, bool bf16, void* ws, hipStream_t st);

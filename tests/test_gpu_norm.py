@@ -1,0 +1,251 @@
+"""The residual stream's norm, its form in 8 bits and its gradient on the GPU against the formulas in 64 bits, and the gradient against differences."""
+import math
+
+import pytest
+import torch
+
+import paper_2503_01840_amd as E
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, FP32 = torch.bfloat16, torch.float32
+U = 2.0 ** -24                                               # half a step of fp32
+EPS = 1e-5
+
+
+def _half(dtype):
+    return 2.0 ** -8 if dtype == BF16 else U
+
+
+# A row's sum of squares: 32 additions in a thread at most, 6 between lanes, 15 between wavefronts, 2 roundings of h in each square: off by
+# 55 U; mean, eps, root and quotient 4 more, of which the root halves what came before: r is off by 32 U.  Then h, h r and gain: 35 U in all
+NORM = 35 * U
+
+
+def _norm(x, gain, residual, eps=EPS):
+    h = x.double() if residual is None else x.double() + residual.double()
+    return gain.double() * h / (h.square().mean(1, keepdim=True) + eps).sqrt(), h
+
+
+def _view(x, how):
+    if how == "dense":
+        return x
+    n, d = x.shape
+    off = 8 if how == "apart" else 1
+    wide = torch.full((n, d + 24), 5.0, dtype=x.dtype, device=x.device)
+    wide[:, off:off + d] = x
+    return wide[:, off:off + d]
+
+
+TYPES = [(BF16, BF16, BF16), (BF16, FP32, BF16), (FP32, FP32, FP32), (FP32, FP32, BF16), (BF16, BF16, FP32), (BF16, FP32, FP32)]      # x, stream, norm
+SIZES = [(1, 1), (1, 8192), (3, 64), (5, 127), (4, 4096), (60, 250), (1025, 72), (1030, 1000), (2, 16384), (2, 16383), (1100, 2056), (7, 4104), (1024, 8192)]
+
+
+@pytest.mark.parametrize("how", ["dense", "apart", "off"])
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("rows,dim", SIZES)
+def test_norm_and_sum(rows, dim, types, how):
+    xt, ht, yt = types
+    g = torch.Generator().manual_seed(rows + dim)
+    x = _view(torch.randn(rows, dim, generator=g).to(xt).to(DEV), how)
+    res = _view((3 * torch.randn(rows, dim, generator=g)).to(ht).to(DEV), how)
+    for gain_t in (BF16, FP32):
+        gain = (1 + 0.2 * torch.randn(dim, generator=g)).to(gain_t).to(DEV)
+        y, h = E.eagle3_add_norm(x, gain, EPS, residual=res, dtype=yt)
+        want, hw = _norm(x, gain, res)
+        assert y.dtype == yt and h.dtype == ht
+        assert bool(((h.double() - hw).abs() <= hw.abs() * (U + _half(ht) * (1 + U))).all())
+        assert bool(((y.double() - want).abs() <= want.abs() * (NORM + _half(yt) * (1 + NORM))).all())
+        if xt == ht:
+            alone = E.eagle3_add_norm(x, gain, EPS, dtype=yt)
+            want, _ = _norm(x, gain, None)
+            assert bool(((alone.double() - want).abs() <= want.abs() * (NORM + _half(yt) * (1 + NORM))).all())
+    # in place: the sum over the residual, the norm over x
+    a, b = _view(x.clone(), how), _view(res.clone(), how)
+    got = E.eagle3_add_norm(a, gain, EPS, residual=b, dtype=xt, out=(a, b))
+    assert got[0] is a and got[1] is b and torch.equal(b, h)
+    assert torch.equal(a, E.eagle3_add_norm(x, gain, EPS, residual=res, dtype=xt)[0])
+    if how != "dense":                                        # nothing but the rows is written
+        off = 8 if how == "apart" else 1
+        for t in (a, b):
+            around = t.as_strided((rows, dim + 24), (dim + 24, 1), t.storage_offset() - off)
+            assert bool((around[:, :off] == 5).all()) and bool((around[:, off + dim:] == 5).all())
+
+
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("types", [(BF16, BF16), (BF16, FP32), (FP32, FP32)])
+@pytest.mark.parametrize("rows,dim", [(1, 1), (1, 8192), (3, 64), (5, 127), (4, 4096), (60, 250), (1025, 72), (1030, 1000), (2, 16384), (2, 16383), (33, 129), (1100, 2056), (9, 136)])
+def test_norm_in_8_bits(rows, dim, types, group):
+    xt, ht = types
+    g = torch.Generator().manual_seed(rows + dim)
+    x, res = torch.randn(rows, dim, generator=g).to(xt).to(DEV), (3 * torch.randn(rows, dim, generator=g)).to(ht).to(DEV)
+    gain = (1 + 0.2 * torch.randn(dim, generator=g)).to(xt).to(DEV)
+    for residual in (res, None):
+        if residual is None and xt != ht:
+            continue
+        got = E.eagle3_add_norm_codes(x, gain, EPS, residual=residual, group=group)
+        codes, scales = got[:2]
+        want, h = _norm(x, gain, residual)
+        n = -(-dim // 128) if group else 1
+        assert codes.dtype == torch.float8_e4m3fn and codes.shape == x.shape and scales.shape == (rows, n)
+        if residual is not None:
+            assert torch.equal(got[2], E.eagle3_add_norm(x, gain, EPS, residual=residual)[1])
+        wide = torch.nn.functional.pad(want, (0, n * (128 if group else dim) - dim)).view(rows, n, -1)
+        s = (wide.abs().amax(2) / 448).clamp(min=2.0 ** -100)
+        assert bool(((scales.double() - s).abs() <= s * (NORM + U)).all())
+        # a code is the nearest one to the value under its scale, which is off by NORM, the reciprocal's two roundings and the product's
+        q = (wide / scales.double()[..., None]).view(rows, -1)[:, :dim]
+        step = torch.exp2(torch.floor(torch.log2(q.abs().clamp(min=2.0 ** -6))) - 3)
+        c = codes.float().double()
+        assert bool(((c - q).abs() <= step / 2 + q.abs() * (2 * NORM + 4 * U)).all()) and bool((c.abs() <= 448).all())
+
+
+def test_codes_of_rows_that_hold_no_numbers_or_nothing():
+    """Zeros, tiny values, one huge one, infinities and NaN."""
+    for dim in (256, 250):
+        x = torch.randn(8, dim, generator=torch.Generator().manual_seed(1)).to(DEV)
+        x[0] = 0
+        x[1] *= 1e-30
+        x[2, 5] = 1e30
+        x[3, 7], x[4, 200] = float("inf"), float("nan")
+        for group in (0, 128):
+            codes, scales = E.eagle3_add_norm_codes(x, torch.ones(dim, device=DEV), 0.0 if group else EPS, group=group)
+            codes, scales = codes.float().cpu(), scales.cpu()
+            assert bool(torch.isfinite(scales).all()) and bool((scales >= 2.0 ** -100).all())
+            if not group:                                     # mean 0: with eps 0 the row is 0 / 0
+                assert bool((codes[0] == 0).all()) and bool((scales[0] == 2.0 ** -100).all())
+            else:
+                assert bool(codes[0].isnan().all())
+            assert bool(codes[4].isnan().all()) and bool(torch.isfinite(codes[5:]).all())
+            assert bool(codes[3, 7].isnan()) and bool((codes[3, :7] == 0).all())       # h r = h * 0, and infinity * 0
+
+
+# Gradient: r as above 32 U; a sum of gain dy h: 2 roundings of each product, 53 additions of magnitudes; r^3, the mean and the products 8 more
+GRAD = 110 * U
+
+
+def _gradient(dy, h, gain, dh, eps=EPS):
+    """(d_sum, d_gain, magnitudes that their errors are measured by)"""
+    dy, h, gain = dy.double(), h.double(), gain.double()
+    r = 1 / (h.square().mean(1, keepdim=True) + eps).sqrt()
+    t = gain * dy * h
+    d = r * gain * dy - h * r ** 3 * t.mean(1, keepdim=True)
+    mag = (r * gain * dy).abs() + h.abs() * r ** 3 * t.abs().mean(1, keepdim=True)
+    if dh is not None:
+        d, mag = d + dh.double(), mag + dh.double().abs()
+    return d, (dy * h * r).sum(0), mag, (dy * h * r).abs().sum(0)
+
+
+@pytest.mark.parametrize("how", ["dense", "apart", "off"])
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("rows,dim", SIZES + [(513, 16), (2050, 13), (40, 6001)])
+def test_gradient(rows, dim, types, how):
+    xt, ht, yt = types
+    g = torch.Generator().manual_seed(rows + dim)
+    h = _view((3 * torch.randn(rows, dim, generator=g)).to(ht).to(DEV), how)
+    dy = _view(torch.randn(rows, dim, generator=g).to(yt).to(DEV), how)
+    dh = _view(torch.randn(rows, dim, generator=g).to(ht).to(DEV), how)
+    for gain_t, more in ((BF16, dh), (FP32, None)):
+        gain = (1 + 0.2 * torch.randn(dim, generator=g)).to(gain_t).to(DEV)
+        dx, d_sum, d_gain = E.eagle3_add_norm_grad(dy, h, gain, EPS, dh=more, x_dtype=xt)
+        assert dx.dtype == xt and d_sum.dtype == ht and d_gain.dtype == gain_t and (dx is d_sum) == (xt == ht)
+        want, want_gain, mag, mag_gain = _gradient(dy, h, gain, more)
+        for got in (dx, d_sum):
+            assert bool(((got.double() - want).abs() <= GRAD * mag + _half(got.dtype) * (want.abs() + GRAD * mag)).all())
+        err = mag_gain * (rows + 40) * U                      # any order of the rows' additions; r, h r and the product
+        assert bool(((d_gain.double() - want_gain).abs() <= err + _half(gain_t) * (want_gain.abs() + err)).all())
+        again = E.eagle3_add_norm_grad(dy, h, gain, EPS, dh=more, x_dtype=xt)
+        assert all(torch.equal(a, b) for a, b in zip((dx, d_sum, d_gain), again))
+
+
+def test_autograd_and_differences():
+    g = torch.Generator().manual_seed(3)
+    rows, dim = 70, 48
+    x, res = (torch.randn(rows, dim, generator=g).to(DEV).requires_grad_() for _ in range(2))
+    gain = (1 + 0.2 * torch.randn(dim, generator=g)).to(DEV).requires_grad_()
+    wy, wh = (torch.randn(rows, dim, generator=g).to(DEV) for _ in range(2))
+    y, h = E.eagle3_add_norm(x, gain, EPS, residual=res)
+    torch.autograd.backward((y, h), (wy, wh))
+    want = E.eagle3_add_norm_grad(wy, h.detach(), gain.detach(), EPS, dh=wh)
+    assert all(torch.equal(a.grad, b) for a, b in zip((x, res, gain), want))
+    # central differences of sum(wy y + wh h) along a direction, step 2^-7: the third derivative's part is some 2^-14 of the gradient's size, and 32-bit results
+    # are off by 40 U of 2 * 70 * 48 values, which the step divides
+    u = [torch.randn(t.shape, generator=g).to(DEV) for t in (x, res, gain)]
+    e = 2.0 ** -7
+
+    def f(sign):
+        with torch.no_grad():
+            a, b = E.eagle3_add_norm(x + sign * e * u[0], gain + sign * e * u[2], EPS, residual=res + sign * e * u[1])
+            return float((wy.double() * a.double()).sum() + (wh.double() * b.double()).sum())
+
+    d = (f(1) - f(-1)) / (2 * e)
+    along = sum(float((t.grad.double() * v.double()).sum()) for t, v in zip((x, res, gain), u))
+    size = sum(float((t.grad.double() * v.double()).abs().sum()) for t, v in zip((x, res, gain), u))
+    assert abs(d - along) <= size * e * e * 4 + float((wy.abs() + wh.abs()).sum()) * 40 * U * 4 / e
+    # one of the two results only; neither norm nor sum of some inputs wanted; mixed types; expanded gradients
+    for t in (x, res, gain):
+        t.grad = None
+    y, h = E.eagle3_add_norm(x, gain, EPS, residual=res)
+    h.backward(wh)
+    assert torch.equal(x.grad, wh) and torch.equal(res.grad, wh) and gain.grad is None
+    x.grad = res.grad = None
+    y, _ = E.eagle3_add_norm(x.detach(), gain.detach(), EPS, residual=res)
+    y.sum().backward()
+    assert torch.equal(res.grad, E.eagle3_add_norm_grad(torch.ones_like(y), (x + res).detach(), gain.detach(), EPS)[1])
+    xb, gb = x.detach().bfloat16().requires_grad_(), gain.detach().bfloat16().requires_grad_()
+    res.grad = None
+    y, h = E.eagle3_add_norm(xb, gb, EPS, residual=res)
+    assert y.dtype == BF16 and h.dtype == FP32
+    torch.autograd.backward((y, h), (wy.bfloat16(), wh))
+    want = E.eagle3_add_norm_grad(wy.bfloat16(), h.detach(), gb.detach(), EPS, dh=wh)
+    assert torch.equal(xb.grad, want[0]) and torch.equal(res.grad, want[1]) and torch.equal(gb.grad, want[2]) and xb.grad.dtype == BF16
+    # without a residual, the norm in another type
+    x.grad = None
+    E.eagle3_add_norm(x, gb, EPS, dtype=BF16).backward(wy.bfloat16())
+    assert torch.equal(x.grad, E.eagle3_add_norm_grad(wy.bfloat16(), x.detach(), gb.detach(), EPS, x_dtype=FP32)[0])
+    with pytest.raises(ValueError):
+        E.eagle3_add_norm(x, gain, EPS, out=torch.empty(rows, dim, device=DEV))
+    y = E.eagle3_add_norm(x, gain, EPS)
+    with torch.no_grad():
+        x += 1
+    with pytest.raises(RuntimeError):
+        y.sum().backward()
+
+
+def test_infinities_stay_in_their_row():
+    x = torch.randn(6, 300, generator=torch.Generator().manual_seed(2)).to(DEV)
+    x[1, 4], x[3, 299] = float("inf"), float("nan")
+    gain, dy = torch.ones(300, device=DEV), torch.ones(6, 300, device=DEV)
+    y = E.eagle3_add_norm(x, gain, EPS)
+    dx = E.eagle3_add_norm_grad(dy, x, gain, EPS)[0]
+    good = [0, 2, 4, 5]
+    assert bool(torch.isfinite(y[good]).all()) and bool(torch.isfinite(dx[good]).all())
+    assert bool(y[3].isnan().all()) and bool(y[1, 4].isnan()) and bool((y[1, :4] == 0).all())
+    assert bool(dx[3].isnan().all())
+
+
+def test_captured_norms_replay():
+    g = torch.Generator().manual_seed(5)
+    x, res, dy = (torch.zeros(900, 264, device=DEV) for _ in range(3))
+    gain = torch.randn(264, generator=g).to(DEV)
+
+    def step():
+        y, h = E.eagle3_add_norm(x, gain, EPS, residual=res)
+        return (y, h, *E.eagle3_add_norm_codes(x, gain, EPS, group=128), *E.eagle3_add_norm_grad(dy, h, gain, EPS, dh=dy))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for i in range(4):
+        for t in (x, res, dy):
+            t.copy_(torch.randn(900, 264, generator=g))
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, want)), i
+        (torch.randn(1000, device=DEV) * 2).sum()
