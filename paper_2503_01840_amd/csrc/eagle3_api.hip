@@ -1001,7 +1001,8 @@ static int distill_rows(int32_t dtype, int32_t rows, int32_t vocab, const void* 
   if (!real_type(dtype) || t->k < 1 || t->k > 1024 || (t->t2d && t->n_t2d < 1) || !(t->temperature > 0.f) || !std::isfinite(t->temperature)) return EAGLE3_E_SHAPE;
   TRY(distill_sizes(rows, vocab));
   if (!rows_fit(logits, stride, vocab, size_of(dtype))) return EAGLE3_E_SHAPE;
-  a = {logits, stride, rows, vocab, t->ids, t->values, t->lse, t->t2d, t->n_t2d, t->k, t->temperature, nullptr, nullptr, nullptr, nullptr, 0};
+  a = {logits, stride, rows, vocab, t->ids, t->values, t->lse, t->t2d, t->n_t2d, t->k, t->temperature, nullptr, nullptr, nullptr, nullptr, 0, 64};
+  while (a.table < 2 * t->k) a.table *= 2;
   return EAGLE3_OK;
 }
 

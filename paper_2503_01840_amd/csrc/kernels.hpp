@@ -309,6 +309,7 @@ struct DistillRows {
   float* stats;             // [rows, 2]
   void* d_logits;
   long long d_stride;
+  int table;                // the kernels' own: places for tokens, a power of two
 };
 size_t distill_workspace(int rows, int vocab);
 hipError_t launch_distill(const DistillRows& a, bool bf16, void* ws, hipStream_t st);
