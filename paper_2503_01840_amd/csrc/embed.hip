@@ -53,6 +53,36 @@ hipError_t rows_of(const EmbedRows& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// ---------------------------------------------------------------- zeros
+// The workgroups behind the first `sorting` ones of every launch that sorts write zeros to the table's blocks from first_block on: sorting keeps few of the chip's
+// units busy.  A table's bytes are pieces of 16 from its first multiple of 16 on, a block's 1024 of them, one to a thread, and less than 16 bytes in front and behind.
+// Workgroups go to the XCDs in turn; each XCD has an eighth of a launch's blocks one behind the other (6.9 TB/s; blocks in turn 6.1, 8192 pieces to a block 5.6).
+constexpr int FILL_PIECES = 1024;
+struct Fill {
+  char* table;
+  size_t bytes;
+  int sorting, first_block, blocks;                           // of this launch: blocks a multiple of 8
+};
+__device__ __forceinline__ void fill(const Fill& f) {
+  const int head = (int)min(f.bytes, (size_t)(-(uintptr_t)f.table & 15)), b = blockIdx.x - f.sorting;
+  const size_t pieces = (f.bytes - head) / 16, block = (size_t)f.first_block + (b & 7) * (f.blocks >> 3) + (b >> 3), p = block * FILL_PIECES + threadIdx.x;
+  const u32x4_t zero = {0, 0, 0, 0};
+  u32x4_t* body = (u32x4_t*)(f.table + head);
+  if (p < pieces) __builtin_nontemporal_store(zero, body + p);
+  if (block == 0) {
+    const int tail = (int)(f.bytes - head - pieces * 16), i = threadIdx.x;
+    if (i < head) f.table[i] = 0;
+    if (i < tail) ((char*)(body + pieces))[i] = 0;
+  }
+}
+// The share of launch number `launch` of `launches`
+void share_out(Fill& f, int launch, int launches) {
+  const size_t eights = f.bytes ? (f.bytes / 16 + 8 * FILL_PIECES - 1) / (8 * FILL_PIECES) + (f.bytes < 16) : 0;
+  const size_t from = eights * launch / launches, to = eights * (launch + 1) / launches;
+  f.first_block = (int)(8 * from);
+  f.blocks = (int)(8 * (to - from));
+}
+
 // ---------------------------------------------------------------- tokens in order
 // A tile of 4096 places to a workgroup of 16 wavefronts: wavefront w has places 256 w + 64 r + lane, r < 4, so that the order of places is that of (w, r, lane).
 constexpr int TILE = 4096, DIGITS = 512;
@@ -63,9 +93,8 @@ __device__ __forceinline__ uint32_t key_of(const int32_t* tokens, int i, int n, 
   return t >= 0 && t < vocab ? (uint32_t)t : (uint32_t)vocab; // padding behind the vocabulary
 }
 
-// The place that each of a tile's keys takes by one digit, in order among equal ones: from base[digit] on (ONE: from the tile's own counts).
-template <bool ONE>
-__device__ __forceinline__ void ranks(const uint32_t* key, int shift, int bits, uint16_t (*count)[DIGITS], uint32_t* base, uint32_t* wave_sums, int* to) {
+// The place that each of a tile's keys takes by one digit, in order among equal ones, from base[digit] on.
+__device__ __forceinline__ void ranks(const uint32_t* key, int shift, int bits, uint16_t (*count)[DIGITS], const uint32_t* base, int* to) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const uint32_t mask = (1u << bits) - 1;
   for (int i = threadIdx.x; i < 16 * DIGITS; i += 1024) count[i / DIGITS][i % DIGITS] = 0;
@@ -88,26 +117,12 @@ __device__ __forceinline__ void ranks(const uint32_t* key, int shift, int bits, 
     __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();
-  // counts of the wavefronts before; the tile's count of a digit
-  uint32_t total = 0;
-  if (threadIdx.x < DIGITS) {
+  if (threadIdx.x < DIGITS) {                                 // counts of the wavefronts before
+    uint32_t total = 0;
     for (int w = 0; w < 16; ++w) {
       const uint32_t c = count[w][threadIdx.x];
       count[w][threadIdx.x] = (uint16_t)total;
       total += c;
-    }
-  }
-  if constexpr (ONE) {                                        // base = sums of the digits below
-    uint32_t sum = total;
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t v = __shfl_up(sum, o, 64);
-      if (lane >= o) sum += v;
-    }
-    if (lane == 63 && wave < DIGITS / 64) wave_sums[wave] = sum;
-    __syncthreads();
-    if (threadIdx.x < DIGITS) {
-      for (int w = 0; w < wave; ++w) sum += wave_sums[w];
-      base[threadIdx.x] = sum - total;
     }
   }
   __syncthreads();
@@ -118,47 +133,42 @@ __device__ __forceinline__ void ranks(const uint32_t* key, int shift, int bits, 
   }
 }
 
-// All of at most TILE places, in one workgroup.
-__global__ __launch_bounds__(1024) void sort_tile_kernel(const int32_t* tokens, int n, int vocab, int passes, int bits, int32_t* token_out, int32_t* row_out) {
-  __shared__ uint16_t count[16][DIGITS];
-  __shared__ uint32_t base[DIGITS], wave_sums[DIGITS / 64];
-  __shared__ uint32_t keys[TILE];
-  __shared__ uint16_t rows[TILE];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  uint32_t key[4];
-  int row[4], to[4];
+// Up to RANKED places: the place of a key is the number of smaller ones and of equal ones in front of it.  A workgroup counts for 64 keys, each of its 16
+// wavefronts a 16th of all others, which it has in scalar registers.
+constexpr int RANKED = 16384;
+__global__ __launch_bounds__(1024) void sort_ranks_kernel(const int32_t* __restrict__ tokens, int n, int vocab, int share, int32_t* token_out, int32_t* row_out, Fill f) {
+  if ((int)blockIdx.x >= f.sorting) return fill(f);
+  __shared__ int counts[16][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i0 = blockIdx.x * 64, i = i0 + lane;
+  const uint32_t key = key_of(tokens, i, n, vocab);
+  const int first = min(n, wave * share), last = min(n, first + share);
+  uint32_t before = 0;
+  // padding has a key of its own behind the others; as an unsigned number it is at least that
+  auto count = [&](int from, int to, uint32_t below) {
+    int j = from;
+    for (; j + 16 <= to; j += 16) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    row[r] = 256 * wave + 64 * r + lane;
-    key[r] = key_of(tokens, row[r], n, vocab);
-  }
-  for (int pass = 0; pass < passes; ++pass) {
-    ranks<true>(key, pass * bits, bits, count, base, wave_sums, to);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      keys[to[r]] = key[r];
-      rows[to[r]] = (uint16_t)row[r];
+      for (int u = 0; u < 16; ++u) before += min((uint32_t)tokens[j + u], (uint32_t)vocab) < below;
     }
-    __syncthreads();
+    for (; j < to; ++j) before += min((uint32_t)tokens[j], (uint32_t)vocab) < below;
+  };
+  count(first, min(last, i0), key + 1);
+  for (int j = max(first, i0); j < min(last, i0 + 64); ++j) before += min((uint32_t)tokens[j], (uint32_t)vocab) < (j < i ? key + 1 : key);
+  count(max(first, i0 + 64), last, key);
+  counts[wave][lane] = (int)before;
+  __syncthreads();
+  if (threadIdx.x < 64 && i < n) {
+    int at = 0;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = 256 * wave + 64 * r + lane;
-      key[r] = keys[i];
-      row[r] = rows[i];
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int i = 256 * wave + 64 * r + lane;
-    if (i < n) {
-      token_out[i] = (int32_t)key[r];
-      row_out[i] = row[r];
-    }
+    for (int w = 0; w < 16; ++w) at += counts[w][lane];
+    token_out[at] = (int32_t)key;
+    row_out[at] = i;
   }
 }
 
 // One digit of more places: a tile's counts, then each tile's places.
-__global__ __launch_bounds__(1024) void sort_count_kernel(const int32_t* tokens, int n, int vocab, int shift, int bits, uint32_t* hist) {
+__global__ __launch_bounds__(1024) void sort_count_kernel(const int32_t* tokens, int n, int vocab, int shift, int bits, uint32_t* hist, Fill f) {
+  if ((int)blockIdx.x >= f.sorting) return fill(f);
   __shared__ uint32_t count[DIGITS];
   if (threadIdx.x < DIGITS) count[threadIdx.x] = 0;
   __syncthreads();
@@ -171,7 +181,8 @@ __global__ __launch_bounds__(1024) void sort_count_kernel(const int32_t* tokens,
   if (threadIdx.x < DIGITS) hist[(size_t)blockIdx.x * DIGITS + threadIdx.x] = count[threadIdx.x];
 }
 __global__ __launch_bounds__(1024) void sort_place_kernel(const int32_t* tokens, const int32_t* rows, int n, int vocab, int shift, int bits, const uint32_t* hist, int tiles,
-                                                          int32_t* token_out, int32_t* row_out) {
+                                                          int32_t* token_out, int32_t* row_out, Fill f) {
+  if ((int)blockIdx.x >= f.sorting) return fill(f);
   __shared__ uint16_t count[16][DIGITS];
   __shared__ uint32_t base[DIGITS], wave_sums[DIGITS / 64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -205,7 +216,7 @@ __global__ __launch_bounds__(1024) void sort_place_kernel(const int32_t* tokens,
     for (int w = 0; w < wave; ++w) sum += wave_sums[w];
     base[threadIdx.x] = sum - all + before;
   }
-  ranks<false>(key, shift, bits, count, base, wave_sums, to);
+  ranks(key, shift, bits, count, base, to);
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int i = blockIdx.x * TILE + 256 * wave + 64 * r + lane;
@@ -217,44 +228,31 @@ __global__ __launch_bounds__(1024) void sort_place_kernel(const int32_t* tokens,
 }
 
 // ---------------------------------------------------------------- sums
-constexpr int CHUNK = 32, BATCH = 8, EMPTY_ROWS = 16;
+constexpr int CHUNK = 16;
 
-// Wavefronts below `sums` sum a chunk's rows for 64 N columns; the others look for tokens that do not occur among EMPTY_ROWS of the table and write zeros.
+// A wavefront sums a chunk's rows for 64 N columns.
 // partial: [chunk][2][dim]: sums of a chunk's first token that began before it, and of its last one that goes on behind it.
 template <typename T, typename O, int N, bool ADD>
-__global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restrict__ token, const int32_t* __restrict__ row_of, int n, int dim, int vocab, EmbedGrad g, int slabs, int sums) {
+__global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restrict__ token, const int32_t* __restrict__ row_of, int n, int dim, int vocab, int slabs, int sums, EmbedGrad g) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int task = blockIdx.x * 4 + wave, pieces = dim / N;
+  if (task >= sums) return;
   O* table = (O*)g.d_table;
-  if (task >= sums) {
-    if (ADD) return;                                          // the rest of the last workgroup
-    const long long v0 = (long long)(task - sums) * EMPTY_ROWS;
-    if (v0 >= vocab) return;
-    // lanes 0..15: does token v0 + lane occur?
-    const int v = (int)min((long long)vocab, v0 + (lane & (EMPTY_ROWS - 1)));
-    int lo = 0, hi = n;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (token[mid] < v) lo = mid + 1;
-      else hi = mid;
-    }
-    const bool absent = v < vocab && !(lo < n && token[lo] == v);
-    const uint64_t empty = __ballot(absent);
-    float zeros[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) zeros[i] = 0.f;
-    for (int i = 0; i < EMPTY_ROWS; ++i) {
-      if (!(empty >> i & 1)) continue;
-      O* to = table + (size_t)(v0 + i) * dim;
-      for (int p = lane; p < pieces; p += 64) store_elems<N>(to + (size_t)p * N, zeros);
-    }
-    return;
+  const int chunk = task / slabs, p = (task - chunk * slabs) * 64 + lane, first = chunk * CHUNK, count = min(n - first, CHUNK);
+  // lane j has the token and row of place first + j; lane CHUNK the token before, the next one that behind, padding (vocab) where there is none
+  int tokens = vocab, rows = 0;
+  if (lane < count) {
+    tokens = token[first + lane];
+    rows = row_of[first + lane];
+  } else if (lane == CHUNK && first > 0) {
+    tokens = token[first - 1];
+  } else if (lane == CHUNK + 1 && first + CHUNK < n) {
+    tokens = token[first + CHUNK];
   }
-  const int chunk = task / slabs, p = (task - chunk * slabs) * 64 + lane, first = chunk * CHUNK, last = min(n, first + CHUNK);
   const bool has = p < pieces;
-  int current = token[first];
+  int current = __builtin_amdgcn_readlane(tokens, 0);
   if (current >= vocab) return;                               // padding only
-  bool began_before = first > 0 && token[first - 1] == current;
+  bool began_before = __builtin_amdgcn_readlane(tokens, CHUNK) == current;
   const T* dy = (const T*)g.dy + (size_t)p * N;
   float sum[N];
 #pragma unroll
@@ -263,8 +261,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restric
   auto leave = [&](bool goes_on) {
     if (!has) return;
     if (began_before || goes_on) {
-      float* to = g.partial + ((size_t)chunk * 2 + (began_before ? 0 : 1)) * dim + (size_t)p * N;
-      store_elems<N>(to, sum);
+      store_elems<N>(g.partial + ((size_t)chunk * 2 + (began_before ? 0 : 1)) * dim + (size_t)p * N, sum);
       return;
     }
     O* to = table + (size_t)current * dim + (size_t)p * N;
@@ -280,30 +277,25 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restric
     }
     store_elems<N>(to, f);
   };
-  for (int at = first; at < last; at += BATCH) {
-    Elems<T, N> e[BATCH];
-    int tok[BATCH];
+  Elems<T, N> e[CHUNK];
 #pragma unroll
-    for (int j = 0; j < BATCH; ++j) {
-      tok[j] = at + j < last ? token[at + j] : vocab;
-      if (tok[j] < vocab && has) e[j].load(dy + (size_t)row_of[at + j] * g.stride);
+  for (int j = 0; j < CHUNK; ++j)                             // places behind the last have row 0, which is not added
+    if (has) e[j].load(dy + (size_t)__builtin_amdgcn_readlane(rows, j) * g.stride);
+#pragma unroll
+  for (int j = 0; j < CHUNK; ++j) {
+    const int next = __builtin_amdgcn_readlane(tokens, j);
+    if (next != current) {
+      leave(false);
+      if (next >= vocab) return;                              // padding, or behind the last place
+      current = next;
+      began_before = false;
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] = 0.f;
     }
 #pragma unroll
-    for (int j = 0; j < BATCH; ++j) {
-      if (at + j >= last) break;
-      if (tok[j] != current) {
-        leave(false);
-        current = tok[j];
-        began_before = false;
-#pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] = 0.f;
-      }
-      if (current >= vocab) return;
-#pragma unroll
-      for (int i = 0; i < N; ++i) sum[i] += has ? e[j].at(i) : 0.f;
-    }
+    for (int i = 0; i < N; ++i) sum[i] += has ? e[j].at(i) : 0.f;
   }
-  leave(last < n && token[last] == current);
+  leave(__builtin_amdgcn_readlane(tokens, CHUNK + 1) == current);
 }
 
 // Tokens whose rows lie in several chunks: workgroup (chunk, 64 N columns) adds the parts of the one that begins in this chunk and goes on behind it, a quarter of
@@ -314,15 +306,16 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restri
   const int chunk = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, p = blockIdx.y * 64 + lane;
   const int first = chunk * CHUNK, end = first + CHUNK;
   if (end >= n) return;
-  const int v = token[end - 1];
-  if (v >= vocab || token[end] != v || (token[first] == v && first > 0 && token[first - 1] == v)) return;
-  int lo = end, hi = n;                                       // behind its last row
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (token[mid] <= v) lo = mid + 1;
-    else hi = mid;
+  const int v = token[end - 1], before = token[max(first, 1) - 1], start = token[first], behind = token[end];
+  if (v >= vocab || behind != v || (start == v && first > 0 && before == v)) return;
+  int parts = 1;                                              // chunks that begin with this token follow each other
+  for (;;) {
+    const long long at = (long long)(chunk + parts + lane) * CHUNK;
+    const uint64_t same = __ballot(at < n && token[at] == v);
+    parts += __popcll(same);
+    if (~same) break;
   }
-  const int parts = (lo - 1) / CHUNK - chunk + 1, share = (parts + 3) / 4;
+  const int share = (parts + 3) / 4;
   const bool has = p < dim / N;
   float sum[N];
 #pragma unroll
@@ -356,27 +349,31 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restri
 size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
 int chunks_of(int rows) { return (rows + CHUNK - 1) / CHUNK; }
 
-// Sorted tokens and their rows, in *token and *row.
-hipError_t sort_tokens(const EmbedGrad& g, char* ws, const int32_t** token, const int32_t** row, hipStream_t st) {
+// Sorted tokens and their rows, in *token and *row, and zeros in the table (f.bytes > 0).
+hipError_t sort_tokens(const EmbedGrad& g, Fill f, char* ws, const int32_t** token, const int32_t** row, hipStream_t st) {
   const int n = g.rows;
-  int bits = 1;                                               // of the largest key, the vocabulary's size
-  while (bits < 31 && g.vocab >> bits) ++bits;
-  const int passes = (bits + 8) / 9, each = (bits + passes - 1) / passes;
   const size_t array = aligned((size_t)n * sizeof(int32_t));
   int32_t* key[2] = {(int32_t*)ws, (int32_t*)(ws + array)};
   int32_t* rows[2] = {(int32_t*)(ws + 2 * array), (int32_t*)(ws + 3 * array)};
-  if (n <= TILE) {
-    hipLaunchKernelGGL(sort_tile_kernel, dim3(1), dim3(1024), 0, st, g.tokens, n, g.vocab, passes, each, key[0], rows[0]);
+  if (n <= RANKED) {
+    f.sorting = (n + 63) / 64;
+    share_out(f, 0, 1);
+    hipLaunchKernelGGL(sort_ranks_kernel, dim3(f.sorting + f.blocks), dim3(1024), 0, st, g.tokens, n, g.vocab, (n + 255) / 256 * 16, key[0], rows[0], f);
     *token = key[0], *row = rows[0];
     return hipGetLastError();
   }
+  int bits = 1;                                               // of the largest key, the vocabulary's size
+  while (bits < 31 && g.vocab >> bits) ++bits;
+  const int passes = (bits + 8) / 9, each = (bits + passes - 1) / passes;
   uint32_t* hist = (uint32_t*)(ws + 4 * array);
-  const int tiles = (n + TILE - 1) / TILE;
+  f.sorting = (n + TILE - 1) / TILE;
   const int32_t* from = g.tokens;
   const int32_t* from_rows = nullptr;
   for (int pass = 0; pass < passes; ++pass) {
-    hipLaunchKernelGGL(sort_count_kernel, dim3(tiles), dim3(1024), 0, st, from, n, g.vocab, pass * each, each, hist);
-    hipLaunchKernelGGL(sort_place_kernel, dim3(tiles), dim3(1024), 0, st, from, from_rows, n, g.vocab, pass * each, each, hist, tiles, key[pass & 1], rows[pass & 1]);
+    share_out(f, 2 * pass, 2 * passes);
+    hipLaunchKernelGGL(sort_count_kernel, dim3(f.sorting + f.blocks), dim3(1024), 0, st, from, n, g.vocab, pass * each, each, hist, f);
+    share_out(f, 2 * pass + 1, 2 * passes);
+    hipLaunchKernelGGL(sort_place_kernel, dim3(f.sorting + f.blocks), dim3(1024), 0, st, from, from_rows, n, g.vocab, pass * each, each, hist, f.sorting, key[pass & 1], rows[pass & 1], f);
     from = key[pass & 1], from_rows = rows[pass & 1];
   }
   *token = from, *row = from_rows;
@@ -386,11 +383,11 @@ hipError_t sort_tokens(const EmbedGrad& g, char* ws, const int32_t** token, cons
 template <typename T, typename O, int N, bool ADD>
 hipError_t sums_of(EmbedGrad g, char* ws, hipStream_t st) {
   const int32_t *token, *row;
-  hipError_t e = sort_tokens(g, ws, &token, &row, st);
+  hipError_t e = sort_tokens(g, {(char*)g.d_table, ADD ? 0 : (size_t)g.vocab * g.dim * sizeof(O), 0, 0, 0}, ws, &token, &row, st);
   if (e != hipSuccess) return e;
   g.partial = (float*)(ws + 4 * aligned((size_t)g.rows * sizeof(int32_t)) + aligned((size_t)((g.rows + TILE - 1) / TILE) * DIGITS * sizeof(uint32_t)));
-  const int slabs = (g.dim / N + 63) / 64, sums = chunks_of(g.rows) * slabs, empty = ADD ? 0 : (g.vocab + EMPTY_ROWS - 1) / EMPTY_ROWS;
-  hipLaunchKernelGGL((embed_sum_kernel<T, O, N, ADD>), dim3((unsigned)(((long long)sums + empty + 3) / 4)), dim3(256), 0, st, token, row, g.rows, g.dim, g.vocab, g, slabs, sums);
+  const int slabs = (g.dim / N + 63) / 64, sums = chunks_of(g.rows) * slabs;
+  hipLaunchKernelGGL((embed_sum_kernel<T, O, N, ADD>), dim3((sums + 3) / 4), dim3(256), 0, st, token, row, g.rows, g.dim, g.vocab, slabs, sums, g);
   e = hipGetLastError();
   if (e != hipSuccess || g.rows <= CHUNK) return e;
   hipLaunchKernelGGL((embed_join_kernel<O, N, ADD>), dim3(chunks_of(g.rows), slabs), dim3(256), 0, st, token, g.rows, g.dim, g.vocab, g);
