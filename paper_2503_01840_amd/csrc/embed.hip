@@ -14,42 +14,42 @@
 namespace {
 
 // ---------------------------------------------------------------- rows
-template <typename T, typename O, int N>
+template <typename T, typename O, bool ODD>
 __global__ __launch_bounds__(256) void embed_kernel(const int32_t* tokens, const T* table, int rows, int dim, int vocab, float scale, O* out, long long stride, int share) {
-  constexpr int U = N == 1 ? 8 : 4;
+  constexpr int U = 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = blockIdx.x * 4 + wave;
   if (r >= rows) return;
-  const int token = tokens[r], pieces = dim / N, first = blockIdx.y * share, last = min(pieces, first + share);
+  const int token = tokens[r], first = blockIdx.y * share, last = min(pieces_of(dim), first + share);
   const bool seen = token >= 0 && token < vocab;
   const T* from = table + (size_t)(seen ? token : 0) * dim;
   O* to = out + (size_t)r * stride;
   for (int p0 = first; p0 < last; p0 += 64 * U) {
-    Elems<T, N> e[U];
+    Piece8<T> e[U];
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int p = p0 + 64 * j + lane;
-      if (seen && p < last) e[j].load(from + (size_t)p * N);
+      if (seen && p < last) e[j].template load<ODD>(from + (size_t)p * PIECE, dim - p * PIECE);
     }
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int p = p0 + 64 * j + lane;
       if (p < last) {
-        float f[N];
+        float f[PIECE];
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = seen ? scale * e[j].at(i) : 0.f;
-        store_elems<N>(to + (size_t)p * N, f);
+        for (int i = 0; i < PIECE; ++i) f[i] = seen ? scale * e[j].at(i) : 0.f;
+        store_piece<ODD>(to + (size_t)p * PIECE, f, dim - p * PIECE);
       }
     }
   }
 }
 
-template <typename T, typename O, int N>
+template <typename T, typename O, bool ODD>
 hipError_t rows_of(const EmbedRows& a, hipStream_t st) {
-  constexpr int U = N == 1 ? 8 : 4;
-  const int most = (a.dim / N + 63) / 64, want = std::max(1, std::min(most, 8192 / a.rows));     // few rows: each over several wavefronts
+  constexpr int U = 4;
+  const int pieces = pieces_of(a.dim), most = (pieces + 63) / 64, want = std::max(1, std::min(most, 8192 / a.rows));     // few rows: each over several wavefronts
   const int each = (most + want - 1) / want, share = 64 * (each > U ? (each + U - 1) / U * U : each);
-  const dim3 grid((a.rows + 3) / 4, (a.dim / N + share - 1) / share);
-  hipLaunchKernelGGL((embed_kernel<T, O, N>), grid, dim3(256), 0, st, a.tokens, (const T*)a.table, a.rows, a.dim, a.vocab, a.scale, (O*)a.out, a.stride, share);
+  const dim3 grid((a.rows + 3) / 4, (pieces + share - 1) / share);
+  hipLaunchKernelGGL((embed_kernel<T, O, ODD>), grid, dim3(256), 0, st, a.tokens, (const T*)a.table, a.rows, a.dim, a.vocab, a.scale, (O*)a.out, a.stride, share);
   return hipGetLastError();
 }
 
@@ -230,12 +230,12 @@ __global__ __launch_bounds__(1024) void sort_place_kernel(const int32_t* tokens,
 // ---------------------------------------------------------------- sums
 constexpr int CHUNK = 16;
 
-// A wavefront sums a chunk's rows for 64 N columns.
-// partial: [chunk][2][dim]: sums of a chunk's first token that began before it, and of its last one that goes on behind it.
-template <typename T, typename O, int N, bool ADD>
+// A wavefront sums a chunk's rows for 64 pieces of columns.
+// partial: [chunk][2][8 pieces_of(dim)]: sums of a chunk's first token that began before it, and of its last one that goes on behind it.
+template <typename T, typename O, bool ODD, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restrict__ token, const int32_t* __restrict__ row_of, int n, int dim, int vocab, int slabs, int sums, EmbedGrad g) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int task = blockIdx.x * 4 + wave, pieces = dim / N;
+  const int task = blockIdx.x * 4 + wave, pieces = pieces_of(dim);
   if (task >= sums) return;
   O* table = (O*)g.d_table;
   const int chunk = task / slabs, p = (task - chunk * slabs) * 64 + lane, first = chunk * CHUNK, count = min(n - first, CHUNK);
@@ -253,34 +253,35 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restric
   int current = __builtin_amdgcn_readlane(tokens, 0);
   if (current >= vocab) return;                               // padding only
   bool began_before = __builtin_amdgcn_readlane(tokens, CHUNK) == current;
-  const T* dy = (const T*)g.dy + (size_t)p * N;
-  float sum[N];
+  const int left = dim - p * PIECE;
+  const T* dy = (const T*)g.dy + (size_t)p * PIECE;
+  float sum[PIECE];
 #pragma unroll
-  for (int i = 0; i < N; ++i) sum[i] = 0.f;
+  for (int i = 0; i < PIECE; ++i) sum[i] = 0.f;
   // what is left of `current` goes to the table, or to the workspace
   auto leave = [&](bool goes_on) {
     if (!has) return;
     if (began_before || goes_on) {
-      store_elems<N>(g.partial + ((size_t)chunk * 2 + (began_before ? 0 : 1)) * dim + (size_t)p * N, sum);
+      store_piece<false>(g.partial + (((size_t)chunk * 2 + (began_before ? 0 : 1)) * pieces + p) * PIECE, sum, PIECE);
       return;
     }
-    O* to = table + (size_t)current * dim + (size_t)p * N;
-    float f[N];
+    O* to = table + (size_t)current * dim + (size_t)p * PIECE;
+    float f[PIECE];
     if constexpr (ADD) {
-      Elems<O, N> old;
-      old.load(to);
+      Piece8<O> old;
+      old.template load<ODD>(to, left);
 #pragma unroll
-      for (int i = 0; i < N; ++i) f[i] = fmaf(g.scale, sum[i], old.at(i));
+      for (int i = 0; i < PIECE; ++i) f[i] = fmaf(g.scale, sum[i], old.at(i));
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) f[i] = g.scale * sum[i];
+      for (int i = 0; i < PIECE; ++i) f[i] = g.scale * sum[i];
     }
-    store_elems<N>(to, f);
+    store_piece<ODD>(to, f, left);
   };
-  Elems<T, N> e[CHUNK];
+  Piece8<T> e[CHUNK];
 #pragma unroll
   for (int j = 0; j < CHUNK; ++j)                             // places behind the last have row 0, which is not added
-    if (has) e[j].load(dy + (size_t)__builtin_amdgcn_readlane(rows, j) * g.stride);
+    if (has) e[j].template load<ODD>(dy + (size_t)__builtin_amdgcn_readlane(rows, j) * g.stride, left);
 #pragma unroll
   for (int j = 0; j < CHUNK; ++j) {
     const int next = __builtin_amdgcn_readlane(tokens, j);
@@ -290,19 +291,19 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restric
       current = next;
       began_before = false;
 #pragma unroll
-      for (int i = 0; i < N; ++i) sum[i] = 0.f;
+      for (int i = 0; i < PIECE; ++i) sum[i] = 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum[i] += has ? e[j].at(i) : 0.f;
+    for (int i = 0; i < PIECE; ++i) sum[i] += has ? e[j].at(i) : 0.f;
   }
   leave(__builtin_amdgcn_readlane(tokens, CHUNK + 1) == current);
 }
 
-// Tokens whose rows lie in several chunks: workgroup (chunk, 64 N columns) adds the parts of the one that begins in this chunk and goes on behind it, a quarter of
+// Tokens whose rows lie in several chunks: workgroup (chunk, 64 pieces of columns) adds the parts of the one that begins in this chunk and goes on behind it, a quarter of
 // them to each wavefront.
-template <typename O, int N, bool ADD>
+template <typename O, bool ODD, bool ADD>
 __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restrict__ token, int n, int dim, int vocab, EmbedGrad g) {
-  __shared__ float part[4][64 * N];
+  __shared__ float part[4][64 * PIECE];
   const int chunk = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, p = blockIdx.y * 64 + lane;
   const int first = chunk * CHUNK, end = first + CHUNK;
   if (end >= n) return;
@@ -316,33 +317,33 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restri
     if (~same) break;
   }
   const int share = (parts + 3) / 4;
-  const bool has = p < dim / N;
-  float sum[N];
+  const bool has = p < pieces_of(dim);
+  float sum[PIECE];
 #pragma unroll
-  for (int i = 0; i < N; ++i) sum[i] = 0.f;
+  for (int i = 0; i < PIECE; ++i) sum[i] = 0.f;
   if (has) {
 #pragma unroll 4
     for (int c = wave * share; c < min(parts, (wave + 1) * share); ++c) {
-      Elems<float, N> e;
-      e.load(g.partial + ((size_t)(chunk + c) * 2 + (c ? 0 : 1)) * dim + (size_t)p * N);
+      Piece8<float> e;
+      e.load<false>(g.partial + (((size_t)(chunk + c) * 2 + (c ? 0 : 1)) * pieces_of(dim) + p) * PIECE, PIECE);
 #pragma unroll
-      for (int i = 0; i < N; ++i) sum[i] += e.at(i);
+      for (int i = 0; i < PIECE; ++i) sum[i] += e.at(i);
     }
   }
 #pragma unroll
-  for (int i = 0; i < N; ++i) part[wave][lane * N + i] = sum[i];
+  for (int i = 0; i < PIECE; ++i) part[wave][lane * PIECE + i] = sum[i];
   __syncthreads();
   if (wave || !has) return;
-  float f[N];
-  O* to = (O*)g.d_table + (size_t)v * dim + (size_t)p * N;
-  Elems<O, N> old;
-  if constexpr (ADD) old.load(to);
+  float f[PIECE];
+  O* to = (O*)g.d_table + (size_t)v * dim + (size_t)p * PIECE;
+  Piece8<O> old;
+  if constexpr (ADD) old.template load<ODD>(to, dim - p * PIECE);
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float s = (part[0][lane * N + i] + part[1][lane * N + i]) + (part[2][lane * N + i] + part[3][lane * N + i]);
+  for (int i = 0; i < PIECE; ++i) {
+    const float s = (part[0][lane * PIECE + i] + part[1][lane * PIECE + i]) + (part[2][lane * PIECE + i] + part[3][lane * PIECE + i]);
     f[i] = ADD ? fmaf(g.scale, s, old.at(i)) : g.scale * s;
   }
-  store_elems<N>(to, f);
+  store_piece<ODD>(to, f, dim - p * PIECE);
 }
 
 // ---------------------------------------------------------------- the workspace: keys and rows, twice, counts, parts
@@ -380,30 +381,30 @@ hipError_t sort_tokens(const EmbedGrad& g, Fill f, char* ws, const int32_t** tok
   return hipGetLastError();
 }
 
-template <typename T, typename O, int N, bool ADD>
+template <typename T, typename O, bool ODD, bool ADD>
 hipError_t sums_of(EmbedGrad g, char* ws, hipStream_t st) {
   const int32_t *token, *row;
   hipError_t e = sort_tokens(g, {(char*)g.d_table, ADD ? 0 : (size_t)g.vocab * g.dim * sizeof(O), 0, 0, 0}, ws, &token, &row, st);
   if (e != hipSuccess) return e;
   g.partial = (float*)(ws + 4 * aligned((size_t)g.rows * sizeof(int32_t)) + aligned((size_t)((g.rows + TILE - 1) / TILE) * DIGITS * sizeof(uint32_t)));
-  const int slabs = (g.dim / N + 63) / 64, sums = chunks_of(g.rows) * slabs;
-  hipLaunchKernelGGL((embed_sum_kernel<T, O, N, ADD>), dim3((sums + 3) / 4), dim3(256), 0, st, token, row, g.rows, g.dim, g.vocab, slabs, sums, g);
+  const int slabs = (pieces_of(g.dim) + 63) / 64, sums = chunks_of(g.rows) * slabs;
+  hipLaunchKernelGGL((embed_sum_kernel<T, O, ODD, ADD>), dim3((sums + 3) / 4), dim3(256), 0, st, token, row, g.rows, g.dim, g.vocab, slabs, sums, g);
   e = hipGetLastError();
   if (e != hipSuccess || g.rows <= CHUNK) return e;
-  hipLaunchKernelGGL((embed_join_kernel<O, N, ADD>), dim3(chunks_of(g.rows), slabs), dim3(256), 0, st, token, g.rows, g.dim, g.vocab, g);
+  hipLaunchKernelGGL((embed_join_kernel<O, ODD, ADD>), dim3(chunks_of(g.rows), slabs), dim3(256), 0, st, token, g.rows, g.dim, g.vocab, g);
   return hipGetLastError();
 }
 
 template <typename T, typename O>
 hipError_t sums_as(const EmbedGrad& g, bool add, char* ws, hipStream_t st) {
-  const bool wide = g.dim % 8 == 0 && rows_at_16(g.dy, g.stride, sizeof(T)) && rows_at_16(g.d_table, g.dim, sizeof(O));
-  if (wide) return add ? sums_of<T, O, 8, true>(g, ws, st) : sums_of<T, O, 8, false>(g, ws, st);
-  return add ? sums_of<T, O, 1, true>(g, ws, st) : sums_of<T, O, 1, false>(g, ws, st);
+  const bool wide = g.dim % PIECE == 0 && rows_at_16(g.dy, g.stride, sizeof(T)) && rows_at_16(g.d_table, g.dim, sizeof(O));
+  if (wide) return add ? sums_of<T, O, false, true>(g, ws, st) : sums_of<T, O, false, false>(g, ws, st);
+  return add ? sums_of<T, O, true, true>(g, ws, st) : sums_of<T, O, true, false>(g, ws, st);
 }
 
 template <typename T, typename O> hipError_t rows_as(const EmbedRows& a, hipStream_t st) {
-  const bool wide = a.dim % 8 == 0 && rows_at_16(a.table, a.dim, sizeof(T)) && rows_at_16(a.out, a.stride, sizeof(O));
-  return wide ? rows_of<T, O, 8>(a, st) : rows_of<T, O, 1>(a, st);
+  const bool wide = a.dim % PIECE == 0 && rows_at_16(a.table, a.dim, sizeof(T)) && rows_at_16(a.out, a.stride, sizeof(O));
+  return wide ? rows_of<T, O, false>(a, st) : rows_of<T, O, true>(a, st);
 }
 
 }  // namespace
@@ -415,7 +416,7 @@ hipError_t launch_embed(const EmbedRows& a, bool table_bf16, bool out_bf16, hipS
 
 size_t embed_grad_workspace(int rows, int dim) {
   return 4 * aligned((size_t)rows * sizeof(int32_t)) + aligned((size_t)((rows + TILE - 1) / TILE) * DIGITS * sizeof(uint32_t)) +
-         (rows > CHUNK ? aligned((size_t)chunks_of(rows) * 2 * dim * sizeof(float)) : 0);
+         (rows > CHUNK ? aligned((size_t)chunks_of(rows) * 2 * pieces_of(dim) * PIECE * sizeof(float)) : 0);
 }
 
 hipError_t launch_embed_grad(const EmbedGrad& g, bool dy_bf16, bool out_bf16, bool add, void* ws, hipStream_t st) {

@@ -287,7 +287,7 @@ struct NormGradRows {
   void* d_sum;
   void* dx;
   void* d_gain;
-  float* partial;           // [NORM_GRAD_PARTS, dim] with d_gain
+  float* partial;           // with d_gain
   long long dy_stride, h_stride, dh_stride, d_sum_stride, dx_stride;
 };
 size_t norm_grad_workspace(int rows, int dim);
