@@ -83,7 +83,7 @@ template <typename T, int U> __device__ __forceinline__ void add_pieces(Stat& st
 #pragma unroll
     for (int i = 0; i < R::N; ++i) m = fmaxf(m, R::at(w[j], i));
   }
-  const float at = finite_or_zero(m), mc = at * c;
+  const float at = finite_or_zero(m);
   float s = st.s * exp2_fast((st.m - at) * c), more = 0.f;
 #pragma unroll
   for (int j = 0; j < U; ++j) {

@@ -1,73 +1,70 @@
-// Rows of elements as pieces of eight, in 32 bits each.  Where every row starts at a multiple of 16 bytes and has whole pieces, a piece is loads and stores of 16 bytes.
-// ODD: rows that do not (the same loads and stores, which this GPU also does at multiples of two bytes), the last piece of a row maybe shorter: an element at a time.
+// Rows of elements as pieces of N (8 or 4), in 32 bits each, a piece one load or store of at most 16 bytes, neighbouring lanes' pieces one behind the other: 8 bf16 elements, or 4
+// where an fp32 row is among a kernel's (two stores of 16 bytes 32 apart for 8 of them take 1.5 times as long).  ODD: rows that do not start at multiples of a piece's
+// bytes (the same loads and stores, which this GPU also does at multiples of an element's), or whose last piece is shorter: an element at a time.
 #pragma once
 #include "common.hpp"
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-typedef u32x4_t u32x4_anywhere __attribute__((aligned(2)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef u32x4_t u32x4_anywhere __attribute__((aligned(2)));
 typedef u32x2_t u32x2_anywhere __attribute__((aligned(1)));
+typedef uint32_t u32_anywhere __attribute__((aligned(1)));
 
-constexpr int PIECE = 8;
-__host__ __device__ __forceinline__ int pieces_of(int n) { return (n + PIECE - 1) / PIECE; }
+__host__ __device__ __forceinline__ int pieces_of(int n, int N) { return (n + N - 1) / N; }
 
-template <bool ODD> __device__ __forceinline__ u32x4_t load16(const void* p) {
-  if constexpr (ODD) return *(const u32x4_anywhere*)p;
-  else return *(const u32x4_t*)p;
-}
-template <bool ODD> __device__ __forceinline__ void store16(void* p, u32x4_t v) {
-  if constexpr (ODD) *(u32x4_anywhere*)p = v;
-  else *(u32x4_t*)p = v;
-}
+// words of 4, 8 or 16 bytes
+template <int BYTES> struct Words;
+template <> struct Words<4> { typedef uint32_t type; typedef u32_anywhere anywhere; };
+template <> struct Words<8> { typedef u32x2_t type; typedef u32x2_anywhere anywhere; };
+template <> struct Words<16> { typedef u32x4_t type; typedef u32x4_anywhere anywhere; };
 
-template <typename T> struct Piece8;
-template <> struct Piece8<bf16_t> {
-  u32x4_t w;
-  __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); }
+template <typename T, int N> struct Piece {
+  static constexpr int BYTES = N * sizeof(T);
+  typedef typename Words<BYTES>::type words;
+  words w;
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
   // `left`: elements from p to the end of the row
-  template <bool ODD> __device__ __forceinline__ void load(const bf16_t* p, int left) {
-    if (!ODD || left >= PIECE) {
-      w = load16<ODD>(p);
+  template <bool ODD> __device__ __forceinline__ void load(const T* p, int left) {
+    if constexpr (!ODD) {
+      w = *(const words*)p;
+    } else if (left >= N) {
+      w = *(const typename Words<BYTES>::anywhere*)p;
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = i < left ? __float_as_uint(p[i]) : 0u;
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = (2 * i < left ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+      for (int i = 0; i < N / 2; ++i) w[i] = (2 * i < left ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)p[2 * i + 1] << 16 : 0u);
     }
   }
-};
-template <> struct Piece8<float> {
-  u32x4_t lo, hi;
-  __device__ __forceinline__ float at(int i) const { return __uint_as_float(i < 4 ? lo[i & 3] : hi[i & 3]); }
-  template <bool ODD> __device__ __forceinline__ void load(const float* p, int left) {
-    if (!ODD || left >= PIECE) {
-      lo = load16<ODD>(p);
-      hi = load16<ODD>(p + 4);
+  __device__ __forceinline__ void set(const float* f) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = __float_as_uint(f[i]);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        lo[i] = i < left ? __float_as_uint(p[i]) : 0u;
-        hi[i] = i + 4 < left ? __float_as_uint(p[i + 4]) : 0u;
-      }
+      for (int i = 0; i < N / 2; ++i) w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
     }
   }
 };
 
-template <bool ODD> __device__ __forceinline__ void store_piece(bf16_t* p, const float* f, int left) {
-  if (!ODD || left >= PIECE) {
-    store16<ODD>(p, u32x4_t{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])});
+// STREAM: past the caches, for results that are larger than these
+template <int N, bool ODD, bool STREAM = false, typename T> __device__ __forceinline__ void store_piece(T* p, const float* f, int left) {
+  Piece<T, N> v;
+  v.set(f);
+  if constexpr (!ODD) {
+    typedef typename Piece<T, N>::words words;
+    if constexpr (STREAM) __builtin_nontemporal_store(v.w, (words*)p);
+    else *(words*)p = v.w;
+  } else if (left >= N) {
+    *(typename Words<Piece<T, N>::BYTES>::anywhere*)p = v.w;
   } else {
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i)
-      if (i < left) p[i] = f32_to_bf16(f[i]);
-  }
-}
-template <bool ODD> __device__ __forceinline__ void store_piece(float* p, const float* f, int left) {
-  if (!ODD || left >= PIECE) {
-    store16<ODD>(p, u32x4_t{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
-    store16<ODD>(p + 4, u32x4_t{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])});
-  } else {
-#pragma unroll
-    for (int i = 0; i < PIECE; ++i)
-      if (i < left) p[i] = f[i];
+    for (int i = 0; i < N; ++i)
+      if (i < left) store_from_f32(p, i, f[i]);
   }
 }
 

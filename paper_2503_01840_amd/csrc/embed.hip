@@ -13,43 +13,47 @@
 
 namespace {
 
+// Bytes of a result from which it is stored past the caches, which it would fill: 16384 rows of 4096 in fp32 (256 MiB) 76 -> 51 us, with an addition behind them that reads them
+// 176 -> 169; 64 MiB in bf16 20 -> 17, but with the addition 41 -> 43.
+constexpr size_t STREAMED = (size_t)128 << 20;
+
 // ---------------------------------------------------------------- rows
-template <typename T, typename O, bool ODD>
+template <typename T, typename O, bool ODD, bool STREAM>
 __global__ __launch_bounds__(256) void embed_kernel(const int32_t* tokens, const T* table, int rows, int dim, int vocab, float scale, O* out, long long stride, int share) {
-  constexpr int U = 4;
+  constexpr int N = sizeof(T) + sizeof(O) == 4 ? 8 : 4, U = 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = blockIdx.x * 4 + wave;
   if (r >= rows) return;
-  const int token = tokens[r], first = blockIdx.y * share, last = min(pieces_of(dim), first + share);
+  const int token = tokens[r], first = blockIdx.y * share, last = min(pieces_of(dim, N), first + share);
   const bool seen = token >= 0 && token < vocab;
   const T* from = table + (size_t)(seen ? token : 0) * dim;
   O* to = out + (size_t)r * stride;
   for (int p0 = first; p0 < last; p0 += 64 * U) {
-    Piece8<T> e[U];
+    Piece<T, N> e[U];
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int p = p0 + 64 * j + lane;
-      if (seen && p < last) e[j].template load<ODD>(from + (size_t)p * PIECE, dim - p * PIECE);
+      if (seen && p < last) e[j].template load<ODD>(from + (size_t)p * N, dim - p * N);
     }
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int p = p0 + 64 * j + lane;
       if (p < last) {
-        float f[PIECE];
+        float f[N];
 #pragma unroll
-        for (int i = 0; i < PIECE; ++i) f[i] = seen ? scale * e[j].at(i) : 0.f;
-        store_piece<ODD>(to + (size_t)p * PIECE, f, dim - p * PIECE);
+        for (int i = 0; i < N; ++i) f[i] = seen ? scale * e[j].at(i) : 0.f;
+        store_piece<N, ODD, STREAM>(to + (size_t)p * N, f, dim - p * N);
       }
     }
   }
 }
 
-template <typename T, typename O, bool ODD>
+template <typename T, typename O, bool ODD, bool STREAM>
 hipError_t rows_of(const EmbedRows& a, hipStream_t st) {
-  constexpr int U = 4;
-  const int pieces = pieces_of(a.dim), most = (pieces + 63) / 64, want = std::max(1, std::min(most, 8192 / a.rows));     // few rows: each over several wavefronts
-  const int each = (most + want - 1) / want, share = 64 * (each > U ? (each + U - 1) / U * U : each);
+  constexpr int N = sizeof(T) + sizeof(O) == 4 ? 8 : 4;
+  const int pieces = pieces_of(a.dim, N), most = (pieces + 63) / 64, want = std::max(1, std::min(most, 8192 / a.rows));     // few rows: each over several wavefronts
+  const int share = 64 * std::min(4, (most + want - 1) / want);
   const dim3 grid((a.rows + 3) / 4, (pieces + share - 1) / share);
-  hipLaunchKernelGGL((embed_kernel<T, O, ODD>), grid, dim3(256), 0, st, a.tokens, (const T*)a.table, a.rows, a.dim, a.vocab, a.scale, (O*)a.out, a.stride, share);
+  hipLaunchKernelGGL((embed_kernel<T, O, ODD, STREAM>), grid, dim3(256), 0, st, a.tokens, (const T*)a.table, a.rows, a.dim, a.vocab, a.scale, (O*)a.out, a.stride, share);
   return hipGetLastError();
 }
 
@@ -229,13 +233,15 @@ __global__ __launch_bounds__(1024) void sort_place_kernel(const int32_t* tokens,
 
 // ---------------------------------------------------------------- sums
 constexpr int CHUNK = 16;
+__host__ __device__ __forceinline__ int padded(int dim) { return (dim + 7) & ~7; }
 
 // A wavefront sums a chunk's rows for 64 pieces of columns.
-// partial: [chunk][2][8 pieces_of(dim)]: sums of a chunk's first token that began before it, and of its last one that goes on behind it.
+// partial: [chunk][2][padded(dim)]: sums of a chunk's first token that began before it, and of its last one that goes on behind it.
 template <typename T, typename O, bool ODD, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restrict__ token, const int32_t* __restrict__ row_of, int n, int dim, int vocab, int slabs, int sums, EmbedGrad g) {
+  constexpr int N = sizeof(T) + sizeof(O) == 4 ? 8 : 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int task = blockIdx.x * 4 + wave, pieces = pieces_of(dim);
+  const int task = blockIdx.x * 4 + wave, pieces = pieces_of(dim, N);
   if (task >= sums) return;
   O* table = (O*)g.d_table;
   const int chunk = task / slabs, p = (task - chunk * slabs) * 64 + lane, first = chunk * CHUNK, count = min(n - first, CHUNK);
@@ -253,32 +259,34 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restric
   int current = __builtin_amdgcn_readlane(tokens, 0);
   if (current >= vocab) return;                               // padding only
   bool began_before = __builtin_amdgcn_readlane(tokens, CHUNK) == current;
-  const int left = dim - p * PIECE;
-  const T* dy = (const T*)g.dy + (size_t)p * PIECE;
-  float sum[PIECE];
+  const int left = dim - p * N;
+  const T* dy = (const T*)g.dy + (size_t)p * N;
+  float sum[N];
 #pragma unroll
-  for (int i = 0; i < PIECE; ++i) sum[i] = 0.f;
+  for (int i = 0; i < N; ++i) sum[i] = 0.f;
   // what is left of `current` goes to the table, or to the workspace
   auto leave = [&](bool goes_on) {
     if (!has) return;
     if (began_before || goes_on) {
-      store_piece<false>(g.partial + (((size_t)chunk * 2 + (began_before ? 0 : 1)) * pieces + p) * PIECE, sum, PIECE);
+      float* to = g.partial + ((size_t)chunk * 2 + (began_before ? 0 : 1)) * padded(dim) + (size_t)p * N;
+#pragma unroll
+      for (int i = 0; i < N; i += 4) store_piece<4, false>(to + i, sum + i, 4);
       return;
     }
-    O* to = table + (size_t)current * dim + (size_t)p * PIECE;
-    float f[PIECE];
+    O* to = table + (size_t)current * dim + (size_t)p * N;
+    float f[N];
     if constexpr (ADD) {
-      Piece8<O> old;
+      Piece<O, N> old;
       old.template load<ODD>(to, left);
 #pragma unroll
-      for (int i = 0; i < PIECE; ++i) f[i] = fmaf(g.scale, sum[i], old.at(i));
+      for (int i = 0; i < N; ++i) f[i] = fmaf(g.scale, sum[i], old.at(i));
     } else {
 #pragma unroll
-      for (int i = 0; i < PIECE; ++i) f[i] = g.scale * sum[i];
+      for (int i = 0; i < N; ++i) f[i] = g.scale * sum[i];
     }
-    store_piece<ODD>(to, f, left);
+    store_piece<N, ODD>(to, f, left);
   };
-  Piece8<T> e[CHUNK];
+  Piece<T, N> e[CHUNK];
 #pragma unroll
   for (int j = 0; j < CHUNK; ++j)                             // places behind the last have row 0, which is not added
     if (has) e[j].template load<ODD>(dy + (size_t)__builtin_amdgcn_readlane(rows, j) * g.stride, left);
@@ -291,10 +299,10 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restric
       current = next;
       began_before = false;
 #pragma unroll
-      for (int i = 0; i < PIECE; ++i) sum[i] = 0.f;
+      for (int i = 0; i < N; ++i) sum[i] = 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i) sum[i] += has ? e[j].at(i) : 0.f;
+    for (int i = 0; i < N; ++i) sum[i] += has ? e[j].at(i) : 0.f;
   }
   leave(__builtin_amdgcn_readlane(tokens, CHUNK + 1) == current);
 }
@@ -303,7 +311,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restric
 // them to each wavefront.
 template <typename O, bool ODD, bool ADD>
 __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restrict__ token, int n, int dim, int vocab, EmbedGrad g) {
-  __shared__ float part[4][64 * PIECE];
+  constexpr int N = 4;
+  __shared__ float part[4][64 * N];
   const int chunk = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, p = blockIdx.y * 64 + lane;
   const int first = chunk * CHUNK, end = first + CHUNK;
   if (end >= n) return;
@@ -317,33 +326,33 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restri
     if (~same) break;
   }
   const int share = (parts + 3) / 4;
-  const bool has = p < pieces_of(dim);
-  float sum[PIECE];
+  const bool has = p < pieces_of(dim, N);
+  float sum[N];
 #pragma unroll
-  for (int i = 0; i < PIECE; ++i) sum[i] = 0.f;
+  for (int i = 0; i < N; ++i) sum[i] = 0.f;
   if (has) {
 #pragma unroll 4
     for (int c = wave * share; c < min(parts, (wave + 1) * share); ++c) {
-      Piece8<float> e;
-      e.load<false>(g.partial + (((size_t)(chunk + c) * 2 + (c ? 0 : 1)) * pieces_of(dim) + p) * PIECE, PIECE);
+      Piece<float, N> e;
+      e.template load<false>(g.partial + ((size_t)(chunk + c) * 2 + (c ? 0 : 1)) * padded(dim) + (size_t)p * N, N);
 #pragma unroll
-      for (int i = 0; i < PIECE; ++i) sum[i] += e.at(i);
+      for (int i = 0; i < N; ++i) sum[i] += e.at(i);
     }
   }
 #pragma unroll
-  for (int i = 0; i < PIECE; ++i) part[wave][lane * PIECE + i] = sum[i];
+  for (int i = 0; i < N; ++i) part[wave][lane * N + i] = sum[i];
   __syncthreads();
   if (wave || !has) return;
-  float f[PIECE];
-  O* to = (O*)g.d_table + (size_t)v * dim + (size_t)p * PIECE;
-  Piece8<O> old;
-  if constexpr (ADD) old.template load<ODD>(to, dim - p * PIECE);
+  float f[N];
+  O* to = (O*)g.d_table + (size_t)v * dim + (size_t)p * N;
+  Piece<O, N> old;
+  if constexpr (ADD) old.template load<ODD>(to, dim - p * N);
 #pragma unroll
-  for (int i = 0; i < PIECE; ++i) {
-    const float s = (part[0][lane * PIECE + i] + part[1][lane * PIECE + i]) + (part[2][lane * PIECE + i] + part[3][lane * PIECE + i]);
+  for (int i = 0; i < N; ++i) {
+    const float s = (part[0][lane * N + i] + part[1][lane * N + i]) + (part[2][lane * N + i] + part[3][lane * N + i]);
     f[i] = ADD ? fmaf(g.scale, s, old.at(i)) : g.scale * s;
   }
-  store_piece<ODD>(to, f, dim - p * PIECE);
+  store_piece<N, ODD>(to, f, dim - p * N);
 }
 
 // ---------------------------------------------------------------- the workspace: keys and rows, twice, counts, parts
@@ -387,24 +396,26 @@ hipError_t sums_of(EmbedGrad g, char* ws, hipStream_t st) {
   hipError_t e = sort_tokens(g, {(char*)g.d_table, ADD ? 0 : (size_t)g.vocab * g.dim * sizeof(O), 0, 0, 0}, ws, &token, &row, st);
   if (e != hipSuccess) return e;
   g.partial = (float*)(ws + 4 * aligned((size_t)g.rows * sizeof(int32_t)) + aligned((size_t)((g.rows + TILE - 1) / TILE) * DIGITS * sizeof(uint32_t)));
-  const int slabs = (pieces_of(g.dim) + 63) / 64, sums = chunks_of(g.rows) * slabs;
+  constexpr int N = sizeof(T) + sizeof(O) == 4 ? 8 : 4;
+  const int slabs = (pieces_of(g.dim, N) + 63) / 64, sums = chunks_of(g.rows) * slabs;
   hipLaunchKernelGGL((embed_sum_kernel<T, O, ODD, ADD>), dim3((sums + 3) / 4), dim3(256), 0, st, token, row, g.rows, g.dim, g.vocab, slabs, sums, g);
   e = hipGetLastError();
   if (e != hipSuccess || g.rows <= CHUNK) return e;
-  hipLaunchKernelGGL((embed_join_kernel<O, ODD, ADD>), dim3(chunks_of(g.rows), slabs), dim3(256), 0, st, token, g.rows, g.dim, g.vocab, g);
+  hipLaunchKernelGGL((embed_join_kernel<O, ODD, ADD>), dim3(chunks_of(g.rows), (g.dim + 255) / 256), dim3(256), 0, st, token, g.rows, g.dim, g.vocab, g);
   return hipGetLastError();
 }
 
 template <typename T, typename O>
 hipError_t sums_as(const EmbedGrad& g, bool add, char* ws, hipStream_t st) {
-  const bool wide = g.dim % PIECE == 0 && rows_at_16(g.dy, g.stride, sizeof(T)) && rows_at_16(g.d_table, g.dim, sizeof(O));
+  const bool wide = g.dim % 8 == 0 && rows_at_16(g.dy, g.stride, sizeof(T)) && rows_at_16(g.d_table, g.dim, sizeof(O));
   if (wide) return add ? sums_of<T, O, false, true>(g, ws, st) : sums_of<T, O, false, false>(g, ws, st);
   return add ? sums_of<T, O, true, true>(g, ws, st) : sums_of<T, O, true, false>(g, ws, st);
 }
 
 template <typename T, typename O> hipError_t rows_as(const EmbedRows& a, hipStream_t st) {
-  const bool wide = a.dim % PIECE == 0 && rows_at_16(a.table, a.dim, sizeof(T)) && rows_at_16(a.out, a.stride, sizeof(O));
-  return wide ? rows_of<T, O, false>(a, st) : rows_of<T, O, true>(a, st);
+  const bool wide = a.dim % 8 == 0 && rows_at_16(a.table, a.dim, sizeof(T)) && rows_at_16(a.out, a.stride, sizeof(O));
+  if (!wide) return rows_of<T, O, true, false>(a, st);
+  return (size_t)a.rows * a.dim * sizeof(O) >= STREAMED ? rows_of<T, O, false, true>(a, st) : rows_of<T, O, false, false>(a, st);
 }
 
 }  // namespace
@@ -416,7 +427,7 @@ hipError_t launch_embed(const EmbedRows& a, bool table_bf16, bool out_bf16, hipS
 
 size_t embed_grad_workspace(int rows, int dim) {
   return 4 * aligned((size_t)rows * sizeof(int32_t)) + aligned((size_t)((rows + TILE - 1) / TILE) * DIGITS * sizeof(uint32_t)) +
-         (rows > CHUNK ? aligned((size_t)chunks_of(rows) * 2 * pieces_of(dim) * PIECE * sizeof(float)) : 0);
+         (rows > CHUNK ? aligned((size_t)chunks_of(rows) * 2 * padded(dim) * sizeof(float)) : 0);
 }
 
 hipError_t launch_embed_grad(const EmbedGrad& g, bool dy_bf16, bool out_bf16, bool add, void* ws, hipStream_t st) {

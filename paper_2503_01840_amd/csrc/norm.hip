@@ -4,7 +4,8 @@
 // them, and the row is written as h and as gain * h / sqrt(mean + eps).  The gradient's rows go to at most 512 workgroups in turn, which keep the gains' gradient in
 // registers; their parts are added by a second launch (4 us).  Bound by bytes, at a large copy's rate and above where rows are many: 16384 rows of 8192 in bf16 178 us
 // (6.0 TB/s), 8192 of 4096 onto an fp32 stream 72 (5.6), 2048 of 8192 in 8 bits 24 (4.9), the gradient of 8191 rows of 4096 on an fp32 stream 102 (5.3).
-// Measured and not kept: an eighth of the rows to each XCD (2 to 17 % slower), the gradient's next row asked for while one is worked on (0 to 8 % slower).
+// Measured and not kept: an eighth of the rows to each XCD (2 to 17 % slower); the gradient's next row asked for while one is worked on (0 to 8 % slower); results stored past the
+// caches (2 to 10 % faster alone, but with an addition behind it that reads them 4096 rows of 8192 in bf16 72 -> 79 us).
 #include <algorithm>
 
 #include "elements.hpp"
@@ -13,7 +14,9 @@
 namespace {
 
 constexpr float CODE_MOST = 448.f, LEAST_SCALE = 0x1p-100f;
+__host__ __device__ __forceinline__ int padded(int dim) { return (dim + 7) & ~7; }
 constexpr int MANY_ROWS = 1024;
+template <typename X, typename H, typename Y> constexpr int piece_size() { return sizeof(X) == 4 || sizeof(H) == 4 || sizeof(Y) == 4 ? 4 : 8; }
 
 // The sum over the 2^lg threads of a row (8 to 1024, neighbours), the same on each; wavefronts in order, `red` a place for each of the workgroup's.
 __device__ __forceinline__ float wave_part_sum(float v, int lg) {
@@ -35,18 +38,21 @@ __device__ __forceinline__ float row_sum(float v, int lg, float* red) {
   return v;
 }
 
-template <bool ODD> __device__ __forceinline__ void load_gains(const NormRows& a, int p, float* g) {
-  const int left = a.dim - p * PIECE;
+template <bool ODD, int N> __device__ __forceinline__ void load_gains(const NormRows& a, int p, float* g) {
+  const int left = a.dim - p * N;
   if (a.gain_bf16) {
-    Piece8<bf16_t> w;
-    w.load<ODD>((const bf16_t*)a.gain + p * PIECE, left);
+    Piece<bf16_t, N> w;
+    w.template load<ODD>((const bf16_t*)a.gain + p * N, left);
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i) g[i] = w.at(i);
+    for (int i = 0; i < N; ++i) g[i] = w.at(i);
   } else {
-    Piece8<float> w;
-    w.load<ODD>((const float*)a.gain + p * PIECE, left);
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i) g[i] = w.at(i);
+    for (int k = 0; k < N; k += 4) {
+      Piece<float, 4> w;
+      w.template load<ODD>((const float*)a.gain + p * N + k, left - k);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[k + i] = w.at(i);
+    }
   }
 }
 
@@ -70,20 +76,21 @@ __device__ __forceinline__ uint32_t to_codes(float a, float b, float inv) {
 template <typename X, typename H, typename Y, bool ADDED, bool ODD, int P>
 __global__ __launch_bounds__(1024) void add_norm_kernel(NormRows a, int lg) {
   constexpr bool CODES = sizeof(Y) == 1;
+  constexpr int N = piece_size<X, H, Y>();
   __shared__ float red[16], most[CODES ? 16 : 1];
   const int per = blockDim.x >> lg, t = threadIdx.x & ((1 << lg) - 1);
   const long long row = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * per + (threadIdx.x >> lg);
-  const int pieces = row < a.rows ? pieces_of(a.dim) : 0;
-  Piece8<X> x[P];
-  Piece8<H> res[P];
-  float h[P][PIECE];
+  const int pieces = row < a.rows ? pieces_of(a.dim, N) : 0;
+  Piece<X, N> x[P];
+  Piece<H, N> res[P];
+  float h[P][N];
   float sum = 0.f;
 #pragma unroll
   for (int j = 0; j < P; ++j) {
     const int p = t + (j << lg);
     if (p < pieces) {
-      x[j].template load<ODD>((const X*)a.x + row * a.x_stride + (long long)p * PIECE, a.dim - p * PIECE);
-      if constexpr (ADDED) res[j].template load<ODD>((const H*)a.residual + row * a.residual_stride + (long long)p * PIECE, a.dim - p * PIECE);
+      x[j].template load<ODD>((const X*)a.x + row * a.x_stride + (long long)p * N, a.dim - p * N);
+      if constexpr (ADDED) res[j].template load<ODD>((const H*)a.residual + row * a.residual_stride + (long long)p * N, a.dim - p * N);
     }
   }
 #pragma unroll
@@ -91,12 +98,12 @@ __global__ __launch_bounds__(1024) void add_norm_kernel(NormRows a, int lg) {
     const int p = t + (j << lg);
     if (p < pieces) {
 #pragma unroll
-      for (int i = 0; i < PIECE; ++i) {
+      for (int i = 0; i < N; ++i) {
         h[j][i] = x[j].at(i);
         if constexpr (ADDED) h[j][i] += res[j].at(i);
         sum = fmaf(h[j][i], h[j][i], sum);
       }
-      if constexpr (ADDED) store_piece<ODD>((H*)a.sum_out + row * a.sum_stride + (long long)p * PIECE, h[j], a.dim - p * PIECE);
+      if constexpr (ADDED) store_piece<N, ODD>((H*)a.sum_out + row * a.sum_stride + (long long)p * N, h[j], a.dim - p * N);
     }
   }
   const float r = 1.f / sqrtf(row_sum(sum, lg, red) / (float)a.dim + a.eps);
@@ -105,11 +112,11 @@ __global__ __launch_bounds__(1024) void add_norm_kernel(NormRows a, int lg) {
     for (int j = 0; j < P; ++j) {
       const int p = t + (j << lg);
       if (p < pieces) {
-        float g[PIECE];
-        load_gains<ODD>(a, p, g);
+        float g[N];
+        load_gains<ODD, N>(a, p, g);
 #pragma unroll
-        for (int i = 0; i < PIECE; ++i) g[i] *= h[j][i] * r;
-        store_piece<ODD>((Y*)a.out + row * a.out_stride + (long long)p * PIECE, g, a.dim - p * PIECE);
+        for (int i = 0; i < N; ++i) g[i] *= h[j][i] * r;
+        store_piece<N, ODD>((Y*)a.out + row * a.out_stride + (long long)p * N, g, a.dim - p * N);
       }
     }
   } else {
@@ -120,16 +127,17 @@ __global__ __launch_bounds__(1024) void add_norm_kernel(NormRows a, int lg) {
       const int p = t + (j << lg);
       part[j] = 0.f;
       if (p < pieces) {
-        float g[PIECE];
-        load_gains<ODD>(a, p, g);
+        float g[N];
+        load_gains<ODD, N>(a, p, g);
 #pragma unroll
-        for (int i = 0; i < PIECE; ++i) {
+        for (int i = 0; i < N; ++i) {
           h[j][i] = g[i] * (h[j][i] * r);
-          if (!ODD || i < a.dim - p * PIECE) part[j] = fmaxf(part[j], finite_magnitude(h[j][i]));
+          if (!ODD || i < a.dim - p * N) part[j] = fmaxf(part[j], finite_magnitude(h[j][i]));
         }
       }
-      if (a.group) {                                          // 16 lanes have a group (lg > 3)
+      if (a.group) {                                          // 128 / N lanes have a group
         part[j] = xlane_max_step<3>(xlane_max_step<2>(xlane_max_step<1>(xlane_max_step<0>(part[j]))));
+        if constexpr (N == 4) part[j] = xlane_max_step<4>(part[j]);
       } else {
         amax = fmaxf(amax, part[j]);
       }
@@ -150,54 +158,55 @@ __global__ __launch_bounds__(1024) void add_norm_kernel(NormRows a, int lg) {
       const int p = t + (j << lg);
       if (p >= pieces) continue;
       const float scale = scale_of(a.group ? part[j] : amax), inv = 1.f / scale;
-      if (a.group ? p % 16 == 0 : p == 0) a.scales[row * n_scales + (a.group ? p / 16 : 0)] = scale;
-      uint8_t* to = (uint8_t*)a.out + row * a.out_stride + (long long)p * PIECE;
-      u32x2_t c;
-      c.x = to_codes(h[j][0], h[j][1], inv) | to_codes(h[j][2], h[j][3], inv) << 16;
-      c.y = to_codes(h[j][4], h[j][5], inv) | to_codes(h[j][6], h[j][7], inv) << 16;
+      if (a.group ? p * N % 128 == 0 : p == 0) a.scales[row * n_scales + (a.group ? p * N / 128 : 0)] = scale;
+      uint8_t* to = (uint8_t*)a.out + row * a.out_stride + (long long)p * N;
+      typename Words<N>::type c;
+      if constexpr (N == 8) c = u32x2_t{to_codes(h[j][0], h[j][1], inv) | to_codes(h[j][2], h[j][3], inv) << 16, to_codes(h[j][4], h[j][5], inv) | to_codes(h[j][6], h[j][7], inv) << 16};
+      else c = to_codes(h[j][0], h[j][1], inv) | to_codes(h[j][2], h[j][3], inv) << 16;
       if constexpr (!ODD) {
-        *(u32x2_t*)to = c;
-      } else if (a.dim - p * PIECE >= PIECE) {
-        *(u32x2_anywhere*)to = c;
+        *(typename Words<N>::type*)to = c;
+      } else if (a.dim - p * N >= N) {
+        *(typename Words<N>::anywhere*)to = c;
       } else {
 #pragma unroll
-        for (int i = 0; i < PIECE; ++i)
-          if (i < a.dim - p * PIECE) to[i] = (uint8_t)((i < 4 ? c.x : c.y) >> 8 * (i & 3));
+        for (int i = 0; i < N; ++i)
+          if (i < a.dim - p * N) to[i] = (uint8_t)(((const uint32_t*)&c)[i / 4] >> 8 * (i & 3));
       }
     }
   }
 }
 
-// Gradient of the sum, rows dealt out in turn; the gains' gradient of a workgroup's rows to its part of the workspace, 8 pieces_of(dim) apart.  dynamic LDS: that many floats
+// Gradient of the sum, rows dealt out in turn; the gains' gradient of a workgroup's rows to its part of the workspace, padded(dim) apart.  dynamic LDS: that many floats
 // where a workgroup has several rows at a time.
 template <typename X, typename H, typename Y, bool ODD, int P>
 __global__ __launch_bounds__(1024) void add_norm_grad_kernel(NormGradRows b, int lg) {
+  constexpr int N = piece_size<X, H, Y>();
   extern __shared__ float gains[];
   __shared__ float red[2][2][16];
   const NormRows& a = b.fwd;
-  const int wave = threadIdx.x >> 6, per = blockDim.x >> lg, group = threadIdx.x >> lg, t = threadIdx.x & ((1 << lg) - 1), all = pieces_of(a.dim);
-  float g[P][PIECE], dg[P][PIECE];
+  const int wave = threadIdx.x >> 6, per = blockDim.x >> lg, group = threadIdx.x >> lg, t = threadIdx.x & ((1 << lg) - 1), all = pieces_of(a.dim, N);
+  float g[P][N], dg[P][N];
 #pragma unroll
   for (int j = 0; j < P; ++j) {
     const int p = t + (j << lg);
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i) g[j][i] = dg[j][i] = 0.f;
-    if (p < all) load_gains<ODD>(a, p, g[j]);
+    for (int i = 0; i < N; ++i) g[j][i] = dg[j][i] = 0.f;
+    if (p < all) load_gains<ODD, N>(a, p, g[j]);
   }
   int turn = 0;
   for (long long r0 = (long long)blockIdx.x * per; r0 < a.rows; r0 += (long long)gridDim.x * per, turn ^= 1) {
     const long long row = r0 + group;
     const int pieces = row < a.rows ? all : 0;
-    Piece8<Y> dy[P];
-    Piece8<H> h[P], dh[P];
+    Piece<Y, N> dy[P];
+    Piece<H, N> h[P], dh[P];
     float hh = 0.f, gh = 0.f;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       const int p = t + (j << lg);
       if (p < pieces) {
-        dy[j].template load<ODD>((const Y*)b.dy + row * b.dy_stride + (long long)p * PIECE, a.dim - p * PIECE);
-        h[j].template load<ODD>((const H*)b.h + row * b.h_stride + (long long)p * PIECE, a.dim - p * PIECE);
-        if (b.dh) dh[j].template load<ODD>((const H*)b.dh + row * b.dh_stride + (long long)p * PIECE, a.dim - p * PIECE);
+        dy[j].template load<ODD>((const Y*)b.dy + row * b.dy_stride + (long long)p * N, a.dim - p * N);
+        h[j].template load<ODD>((const H*)b.h + row * b.h_stride + (long long)p * N, a.dim - p * N);
+        if (b.dh) dh[j].template load<ODD>((const H*)b.dh + row * b.dh_stride + (long long)p * N, a.dim - p * N);
       }
     }
 #pragma unroll
@@ -205,7 +214,7 @@ __global__ __launch_bounds__(1024) void add_norm_grad_kernel(NormGradRows b, int
       const int p = t + (j << lg);
       if (p < pieces) {
 #pragma unroll
-        for (int i = 0; i < PIECE; ++i) {
+        for (int i = 0; i < N; ++i) {
           hh = fmaf(h[j].at(i), h[j].at(i), hh);
           gh = fmaf(g[j][i] * dy[j].at(i), h[j].at(i), gh);
         }
@@ -232,21 +241,21 @@ __global__ __launch_bounds__(1024) void add_norm_grad_kernel(NormGradRows b, int
     for (int j = 0; j < P; ++j) {
       const int p = t + (j << lg);
       if (p < pieces) {
-        float y[PIECE];
+        float y[N];
 #pragma unroll
-        for (int i = 0; i < PIECE; ++i) {
+        for (int i = 0; i < N; ++i) {
           const float d = dy[j].at(i), v = h[j].at(i);
           y[i] = fmaf(g[j][i] * d, r, -(v * c));
           if (b.dh) y[i] += dh[j].at(i);
           dg[j][i] = fmaf(d, v * r, dg[j][i]);
         }
-        if (b.d_sum) store_piece<ODD>((H*)b.d_sum + row * b.d_sum_stride + (long long)p * PIECE, y, a.dim - p * PIECE);
-        if (b.dx) store_piece<ODD>((X*)b.dx + row * b.dx_stride + (long long)p * PIECE, y, a.dim - p * PIECE);
+        if (b.d_sum) store_piece<N, ODD>((H*)b.d_sum + row * b.d_sum_stride + (long long)p * N, y, a.dim - p * N);
+        if (b.dx) store_piece<N, ODD>((X*)b.dx + row * b.dx_stride + (long long)p * N, y, a.dim - p * N);
       }
     }
   }
   if (!b.partial) return;
-  float* to = b.partial + (size_t)blockIdx.x * all * PIECE;
+  float* to = b.partial + (size_t)blockIdx.x * padded(a.dim);
   if (per > 1) {                                              // rows of a workgroup one after the other
     for (int w = 0; w < per; ++w) {
       if (w == group) {
@@ -255,26 +264,29 @@ __global__ __launch_bounds__(1024) void add_norm_grad_kernel(NormGradRows b, int
           const int p = t + (j << lg);
           if (p < all) {
 #pragma unroll
-            for (int i = 0; i < PIECE; ++i) gains[p * PIECE + i] = (w ? gains[p * PIECE + i] : 0.f) + dg[j][i];
+            for (int i = 0; i < N; ++i) gains[p * N + i] = (w ? gains[p * N + i] : 0.f) + dg[j][i];
           }
         }
       }
       __syncthreads();
     }
-    for (int i = threadIdx.x; i < all * PIECE; i += blockDim.x) to[i] = gains[i];
+    for (int i = threadIdx.x; i < a.dim; i += blockDim.x) to[i] = gains[i];
     return;
   }
 #pragma unroll
   for (int j = 0; j < P; ++j) {
     const int p = t + (j << lg);
-    if (p < all) store_piece<false>(to + p * PIECE, dg[j], PIECE);
+    if (p < all) {
+#pragma unroll
+      for (int i = 0; i < N; i += 4) store_piece<4, false>(to + p * N + i, dg[j] + i, 4);
+    }
   }
 }
 
 // d_gain = the sum of the workgroups' parts, 64 columns to a workgroup of 16 wavefronts.
 __global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, int parts, int dim, bool bf16, void* d_gain) {
   __shared__ float red[16][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = blockIdx.x * 64 + lane, apart = pieces_of(dim) * PIECE;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = blockIdx.x * 64 + lane, apart = padded(dim);
   float s = 0.f;
   if (at < dim) {
 #pragma unroll 8
@@ -290,8 +302,8 @@ __global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, in
 }
 
 // Threads to a row, as a power of two: a piece each up to a wavefront's 64, and where rows are few; up to `most` pieces each where they are many.  One and two, us:
-// 16384 bf16 rows of 8192 178 and 186, 8192 fp32 rows of 4096 93 and 99; 4096 bf16 rows of 2048 12.5 and 10.8; without a residual 16384 rows of 4096 53 and 46; 2048 rows of
-// 8192 in 8 bits 27.7 and 24.0.  The gradient: 16384 rows of 2048 61 and 55.
+// 16384 bf16 rows of 8192 179 and 186, but 4096 of 2048 12.4 and 10.8, and without a residual 16384 of 4096 53 and 46; 2048 rows of 8192 in 8 bits 27.5 and 24.1; 8192 fp32 rows of
+// 4096 90 and 93, onto an fp32 stream 71 and 69.  The gradient: 16384 rows of 2048 62 and 54, four pieces in fp32 8191 rows of 4096 134 and 99.
 int threads_of(int pieces, int most, int rows, int least) {
   const int share = rows >= MANY_ROWS ? most : 1;
   int lg = least;
@@ -309,9 +321,11 @@ hipError_t launch_forward(const NormRows& a, int lg, hipStream_t st) {
 
 template <typename X, typename H, typename Y, bool ADDED, bool ODD>
 hipError_t forward(const NormRows& a, hipStream_t st) {
-  const int pieces = pieces_of(a.dim), lg = threads_of(pieces, ADDED && sizeof(Y) > 1 && pieces >= 512 ? 1 : 2, a.rows, sizeof(Y) == 1 ? 4 : 3), P = (pieces + (1 << lg) - 1) >> lg;
+  constexpr int N = piece_size<X, H, Y>();
+  const int pieces = pieces_of(a.dim, N), lg = threads_of(pieces, N == 8 && ADDED && sizeof(Y) > 1 && pieces >= 1024 ? 1 : 2, a.rows, sizeof(Y) > 1 ? 3 : N == 8 ? 4 : 5), P = (pieces + (1 << lg) - 1) >> lg;
   if (P <= 1) return launch_forward<X, H, Y, ADDED, ODD, 1>(a, lg, st);
-  return launch_forward<X, H, Y, ADDED, ODD, 2>(a, lg, st);
+  if (P <= 2) return launch_forward<X, H, Y, ADDED, ODD, 2>(a, lg, st);
+  return launch_forward<X, H, Y, ADDED, ODD, 4>(a, lg, st);
 }
 
 template <typename X, typename H, typename Y>
@@ -334,7 +348,7 @@ template <typename X, typename H, typename Y, bool ODD, int P>
 hipError_t launch_backward(const NormGradRows& b, int lg, hipStream_t st) {
   const int threads = std::max(256, 1 << lg), per = threads >> lg;
   const int grid = std::min((b.fwd.rows + per - 1) / per, NORM_GRAD_PARTS);
-  hipLaunchKernelGGL((add_norm_grad_kernel<X, H, Y, ODD, P>), dim3(grid), dim3(threads), per > 1 ? pieces_of(b.fwd.dim) * PIECE * sizeof(float) : 0, st, b, lg);
+  hipLaunchKernelGGL((add_norm_grad_kernel<X, H, Y, ODD, P>), dim3(grid), dim3(threads), per > 1 ? padded(b.fwd.dim) * sizeof(float) : 0, st, b, lg);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !b.partial) return e;
   hipLaunchKernelGGL(gain_sum_kernel, dim3((b.fwd.dim + 63) / 64), dim3(1024), 0, st, b.partial, grid, b.fwd.dim, b.fwd.gain_bf16, b.d_gain);
@@ -343,21 +357,27 @@ hipError_t launch_backward(const NormGradRows& b, int lg, hipStream_t st) {
 
 template <typename X, typename H, typename Y, bool ODD>
 hipError_t backward(const NormGradRows& b, hipStream_t st) {
-  const int pieces = pieces_of(b.fwd.dim), lg = threads_of(pieces, 2, b.fwd.rows, 3), P = (pieces + (1 << lg) - 1) >> lg;
+  constexpr int N = piece_size<X, H, Y>();
+  const int pieces = pieces_of(b.fwd.dim, N), lg = threads_of(pieces, 2, b.fwd.rows, 3), P = (pieces + (1 << lg) - 1) >> lg;
   if (P <= 1) return launch_backward<X, H, Y, ODD, 1>(b, lg, st);
-  return launch_backward<X, H, Y, ODD, 2>(b, lg, st);
+  if (P <= 2) return launch_backward<X, H, Y, ODD, 2>(b, lg, st);
+  return launch_backward<X, H, Y, ODD, 4>(b, lg, st);
+}
+
+template <typename X, typename H, typename Y>
+hipError_t backward_as(const NormGradRows& b, bool wide, hipStream_t st) {
+  return wide ? backward<X, H, Y, false>(b, st) : backward<X, H, Y, true>(b, st);
 }
 
 template <typename X, typename H>
 hipError_t backward_types(const NormGradRows& b, int dy_type, bool wide, hipStream_t st) {
-  if (dy_type == NORM_BF16) return wide ? backward<X, H, bf16_t, false>(b, st) : backward<X, H, bf16_t, true>(b, st);
-  return wide ? backward<X, H, float, false>(b, st) : backward<X, H, float, true>(b, st);
+  return dy_type == NORM_BF16 ? backward_as<X, H, bf16_t>(b, wide, st) : backward_as<X, H, float>(b, wide, st);
 }
 
 }  // namespace
 
 hipError_t launch_norm_rows(const NormRows& a, int x_type, int sum_type, int out_type, hipStream_t st) {
-  const bool wide = a.dim % PIECE == 0 && rows_at_16(a.x, a.x_stride, type_size(x_type)) && rows_at_16(a.gain, 0, 1) &&
+  const bool wide = a.dim % 8 == 0 && rows_at_16(a.x, a.x_stride, type_size(x_type)) && rows_at_16(a.gain, 0, 1) &&
                     (!a.residual || (rows_at_16(a.residual, a.residual_stride, type_size(sum_type)) && rows_at_16(a.sum_out, a.sum_stride, type_size(sum_type)))) &&
                     (out_type == NORM_CODES ? ((uintptr_t)a.out | (uintptr_t)a.out_stride) % 8 == 0 : rows_at_16(a.out, a.out_stride, type_size(out_type)));
   if (x_type == NORM_FP32) return forward_types<float, float>(a, out_type, wide, st);
@@ -367,11 +387,11 @@ hipError_t launch_norm_rows(const NormRows& a, int x_type, int sum_type, int out
 hipError_t launch_norm_rows_grad(const NormGradRows& b, int dy_type, int sum_type, int x_type, hipStream_t st) {
   const NormRows& a = b.fwd;
   const int sum_size = type_size(sum_type);
-  const bool wide = a.dim % PIECE == 0 && rows_at_16(a.gain, 0, 1) && rows_at_16(b.dy, b.dy_stride, type_size(dy_type)) && rows_at_16(b.h, b.h_stride, sum_size) &&
+  const bool wide = a.dim % 8 == 0 && rows_at_16(a.gain, 0, 1) && rows_at_16(b.dy, b.dy_stride, type_size(dy_type)) && rows_at_16(b.h, b.h_stride, sum_size) &&
                     (!b.dh || rows_at_16(b.dh, b.dh_stride, sum_size)) && (!b.d_sum || rows_at_16(b.d_sum, b.d_sum_stride, sum_size)) &&
                     (!b.dx || rows_at_16(b.dx, b.dx_stride, type_size(x_type)));
   if (x_type == NORM_FP32) return backward_types<float, float>(b, dy_type, wide, st);
   return sum_type == NORM_FP32 ? backward_types<bf16_t, float>(b, dy_type, wide, st) : backward_types<bf16_t, bf16_t>(b, dy_type, wide, st);
 }
 
-size_t norm_grad_workspace(int rows, int dim) { return ((size_t)std::min(rows, NORM_GRAD_PARTS) * pieces_of(dim) * PIECE * sizeof(float) + 255) / 256 * 256; }
+size_t norm_grad_workspace(int rows, int dim) { return ((size_t)std::min(rows, NORM_GRAD_PARTS) * padded(dim) * sizeof(float) + 255) / 256 * 256; }
