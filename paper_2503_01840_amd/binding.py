@@ -708,12 +708,15 @@ def _workspace(call, sizes, like):
 
 
 def _recorded(*tensors):
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            return torch.is_grad_enabled()
+    return False
 
 
 def _not_over_records(out, *inputs):
     """Results go to new tensors where gradients are recorded."""
-    if out is not None and _recorded(*inputs, *(out if isinstance(out, (tuple, list)) else (out,))):
+    if _recorded(*inputs, *(out if isinstance(out, (tuple, list)) else (out,))):
         _refuse("out", "None where gradients are recorded", out)
 
 
@@ -725,8 +728,10 @@ def _embed(table, tokens, scale, dtype, out):
     rows = tokens.shape[0]
     tok = _arg(tokens, torch.int32, (rows,), gpu, "tokens")
     if out is None:
-        out = table.new_empty((rows, d), dtype=table.dtype if dtype is None else dtype)
-    op, _, _, stride, out_code = _like(out, rows, d, gpu, "out", dtype)
+        out = table.new_empty((rows, d), dtype=dtype)
+        op, stride, out_code = out.data_ptr(), d, code if dtype is None else _TYPES[dtype]
+    else:
+        op, _, _, stride, out_code = _like(out, rows, d, gpu, "out", dtype)
     _on(gpu, lib().eagle3_embed, code, rows, d, V, tp, tok, scale, out_code, op, stride)
     return out
 
@@ -750,8 +755,9 @@ def eagle3_embed(table, tokens, scale=1.0, dtype=None, out=None):
     vocabulary give rows of zeros.  `out`: [rows, dim], rows any distance apart.  Recorded for autograd where the table requires a gradient."""
     if dtype is not None:
         _type(dtype, "dtype")
-    _not_over_records(out, table)
-    if _recorded(table):
+    if out is not None:
+        _not_over_records(out, table)
+    elif table.requires_grad and torch.is_grad_enabled():
         return _Embedded.apply(table, tokens, scale, dtype)
     return _embed(table, tokens, scale, dtype, out)
 
@@ -765,11 +771,15 @@ def eagle3_embed_grad(dy, tokens, vocab, scale=1.0, dtype=None, out=None, accumu
     if out is None:
         if accumulate:
             _refuse("out", "with accumulate what to add to", out)
-        out = dy.new_empty((vocab, d), dtype=dy.dtype if dtype is None else dtype)
-    op, _, _, _, out_code = _like(out, vocab, d, gpu, "out", dtype)
-    if not out.is_contiguous():
-        _refuse("out", "a dense tensor", out)
-    _not_over_records(out)
+        if dtype is not None:
+            _type(dtype, "dtype")
+        out = dy.new_empty((vocab, d), dtype=dtype)
+        op, out_code = out.data_ptr(), code if dtype is None else _TYPES[dtype]
+    else:
+        op, _, _, _, out_code = _like(out, vocab, d, gpu, "out", dtype)
+        if not out.is_contiguous():
+            _refuse("out", "a dense tensor", out)
+        _not_over_records(out)
     ws, size, _keep = _workspace("eagle3_embed_grad_workspace", (rows, d, vocab), dy)
     _on(gpu, lib().eagle3_embed_grad, code, rows, d, vocab, dp, stride, tok, scale, bool(accumulate), out_code, op, ws, size)
     return out
@@ -806,8 +816,10 @@ def _add_norm(x, gain, eps, residual, dtype, out):
     y, h = out if isinstance(out, (tuple, list)) else (out, None)
     h, hp, hs = _sum_out(h, residual, n, d, gpu)
     if y is None:
-        y = x.new_empty((n, d), dtype=x.dtype if dtype is None else dtype)
-    yp, _, _, ys, yc = _like(y, n, d, gpu, "out", dtype)
+        y = x.new_empty((n, d), dtype=dtype)
+        yp, ys, yc = y.data_ptr(), d, xa[2] if dtype is None else _TYPES[dtype]
+    else:
+        yp, _, _, ys, yc = _like(y, n, d, gpu, "out", dtype)
     _on(gpu, lib().eagle3_add_norm, *xa, *ra, hp, hs, *ga, eps, yc, yp, ys)
     return y if residual is None else (y, h)
 
@@ -838,8 +850,9 @@ def eagle3_add_norm(x, gain, eps, residual=None, dtype=None, out=None):
     tensor, or (the norm's or None, the sum's or None), which may be x and residual themselves.  Recorded for autograd, which `out` does not allow."""
     if dtype is not None:
         _type(dtype, "dtype")
-    _not_over_records(out, x, gain, residual)
-    if _recorded(x, gain, residual):
+    if out is not None:
+        _not_over_records(out, x, gain, residual)
+    elif _recorded(x, gain, residual):
         return _Normed.apply(x, gain, eps, residual, dtype)
     return _add_norm(x, gain, eps, residual, dtype, out)
 
@@ -847,9 +860,10 @@ def eagle3_add_norm(x, gain, eps, residual=None, dtype=None, out=None):
 def eagle3_add_norm_codes(x, gain, eps, residual=None, group=0, out=None):
     """The norm of eagle3_add_norm in 8 bits: (codes float8_e4m3fn [rows, dim], scales fp32 [rows, groups]), with residual (codes, scales, h).  group: columns
     to a scale, 128, or 0 for one scale a row.  `out`: the sum's tensor.  Nothing is recorded for autograd."""
+    if out is not None:
+        _not_over_records(out, residual)
     gpu, n, d, xa, ra, ga = _norm_inputs(x, gain, residual)
     h, hp, hs = _sum_out(out, residual, n, d, gpu)
-    _not_over_records(out, residual)
     codes = x.new_empty((n, d), dtype=torch.float8_e4m3fn)
     scales = x.new_empty((n, -(-d // group) if group else 1), dtype=torch.float32)
     _on(gpu, lib().eagle3_add_norm_codes, *xa, *ra, hp, hs, *ga, eps, group, codes.data_ptr(), d, scales.data_ptr())
@@ -921,7 +935,7 @@ def eagle3_distill(logits, ids, values, lse=None, t2d=None, temperature=1.0, wan
     """The cross entropy, fp32 [rows], of a student's logits [rows, vocab] (bf16 or fp32, rows any distance apart) against a teacher's logits `values` fp32 [rows, k] of
     the tokens `ids` int32 [rows, k] (include/eagle3.h: eagle3_teacher): the teacher's probabilities among these tokens, or with lse fp32 [rows] those that it gave
     them; t2d int32 [n]: the student's ids of the teacher's tokens.  With want_stats (loss, stats fp32 [rows, 2]).  Recorded for autograd."""
-    if _recorded(logits):
+    if logits.requires_grad and torch.is_grad_enabled():
         got = _Distilled.apply(logits, ids, values, lse, t2d, temperature)
         return got if want_stats else got[0]
     got = _distill(logits, ids, values, lse, t2d, temperature, want_stats)

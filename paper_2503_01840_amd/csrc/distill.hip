@@ -380,7 +380,7 @@ __global__ __launch_bounds__(THREADS) void distill_grad_kernel(DistillRows a, fl
 
 // Loss and gradient of a row: its first R THREADS pieces stay in registers between the two, the next Q THREADS in LDS (behind the teacher's), what is behind
 // them is read twice.
-template <typename T, int THREADS, int R, int Q, int WAVES>
+template <typename T, int THREADS, int R, int Q, int WAVES, bool EVEN>
 __global__ __launch_bounds__(THREADS, WAVES) void distill_step_kernel(DistillRows a, float c) {
   extern __shared__ uint32_t lds[];
   __shared__ float red[2][16], sum_of_weights;
@@ -420,15 +420,15 @@ __global__ __launch_bounds__(THREADS, WAVES) void distill_step_kernel(DistillRow
   write_single(row, out, any, st, c, k);
   if (threadIdx.x >= THREADS - 64) write_loss(a, r, t, P, st);
   if (!any) {
-    write_zeros<T, THREADS, true>(row, out, 0, row.pieces);
+    write_zeros<T, THREADS, EVEN>(row, out, 0, row.pieces);
     return;
   }
 #pragma unroll
   for (int j = 0; j < R; ++j)
-    if ((int)threadIdx.x < row.pieces - j * THREADS) row.template store_gradient<true>(out, j * THREADS, threadIdx.x, w[j], st.m, c, k);
+    if ((int)threadIdx.x < row.pieces - j * THREADS) row.template store_gradient<EVEN>(out, j * THREADS, threadIdx.x, w[j], st.m, c, k);
   if constexpr (Q > 0)
-    for (int p = R * THREADS + threadIdx.x; p < in_lds; p += THREADS) row.template store_gradient<true>(out, p, 0, kept[p - R * THREADS], st.m, c, k);
-  write_pieces<T, THREADS, true>(row, out, (R + Q) * THREADS, row.pieces, st, c, k);
+    for (int p = R * THREADS + threadIdx.x; p < in_lds; p += THREADS) row.template store_gradient<EVEN>(out, p, 0, kept[p - R * THREADS], st.m, c, k);
+  write_pieces<T, THREADS, EVEN>(row, out, (R + Q) * THREADS, row.pieces, st, c, k);
   __syncthreads();                                            // the tokens' entries behind everybody's
   if (threadIdx.x < 64) write_tokens<T>(a, t, out, 0, a.vocab, a.vocab, a.vocab, st, c, k, g);
 }
@@ -438,8 +438,13 @@ size_t lds_of(const DistillRows& a) { return ((size_t)a.k * 16 + (size_t)a.table
 float factor_of(const DistillRows& a) { return (float)(1.4426950408889634074 / (double)a.temperature); }
 int most_pieces(const DistillRows& a, int size) { return std::max(1, a.vocab / (16 / size)); }       // of a row, wherever it starts
 
-// Parts of a row, so that few rows fill the chip: of at least 1024 pieces
-int parts_of(int rows, int pieces) { return std::max(1, std::min((pieces + 1023) / 1024, 1024 / std::min(rows, 1024))); }
+// Parts of a row, where few rows would leave most of the chip idle.  Gradient: its workgroups are one launch in any case (us, 16384 pieces: 16 rows 6.3 in 16 parts, 12.2 in one;
+// 128 rows 15.4 in four, 16.7; 256 rows 29.8 in four, 23.0 in one).
+int grad_parts(int rows, int pieces) { return rows >= 256 ? 1 : std::max(1, std::min(pieces / 1024, 512 / rows)); }
+// Loss, and loss and gradient in one call: in parts they are two and three launches, which cost the host 3 us each.  16 rows of 16384 pieces: loss 6.6 us in parts and 10.2
+// in one, a call of it 14 and 10; step 12.6 and 17.2; of 32768 pieces 6.7 and 10.2, 14.5 and 19.4; 64 rows 11.6 and 11.5, 23.4 and 22.5.
+int loss_parts(int rows, int pieces) { return rows >= 64 || pieces <= 32768 ? 1 : std::min((pieces + 1023) / 1024, 1024 / rows); }
+int step_parts(int rows, int pieces) { return rows >= 64 || pieces <= 16384 ? 1 : std::min((pieces + 1023) / 1024, 1024 / rows); }
 dim3 grid_of(int rows, int parts) {
   const int x = std::min(rows, 1 << 20);                      // a grid has less than 2^32 threads in one direction
   return dim3(x, (rows + x - 1) / x, parts);
@@ -448,8 +453,8 @@ dim3 grid_of(int rows, int parts) {
 template <typename T, int THREADS> void loss_kernel(const DistillRows& a, const float* partial, int parts, hipStream_t st) {
   hipLaunchKernelGGL((distill_loss_kernel<T, THREADS>), grid_of(a.rows, 1), dim3(THREADS), lds_of(a), st, a, factor_of(a), partial, parts);
 }
-template <typename T> hipError_t loss_rows(const DistillRows& a, void* ws, hipStream_t st) {
-  const int pieces = most_pieces(a, sizeof(T)), parts = parts_of(a.rows, pieces);
+template <typename T> hipError_t loss_rows(const DistillRows& a, int parts, void* ws, hipStream_t st) {
+  const int pieces = most_pieces(a, sizeof(T));
   if (parts > 1) {
     hipLaunchKernelGGL((distill_part_kernel<T, 256>), grid_of(a.rows, parts), dim3(256), 0, st, a, factor_of(a), (pieces + parts - 1) / parts, (float*)ws);
     loss_kernel<T, 64>(a, (const float*)ws, parts, st);
@@ -457,8 +462,10 @@ template <typename T> hipError_t loss_rows(const DistillRows& a, void* ws, hipSt
     loss_kernel<T, 64>(a, nullptr, 0, st);
   } else if (pieces <= 512) {
     loss_kernel<T, 128>(a, nullptr, 0, st);
-  } else {
+  } else if (pieces <= 2048) {
     loss_kernel<T, 256>(a, nullptr, 0, st);
+  } else {
+    loss_kernel<T, 512>(a, nullptr, 0, st);
   }
   return hipGetLastError();
 }
@@ -475,7 +482,7 @@ template <typename T, int THREADS, int R> hipError_t grad_kernel(const DistillRo
   return hipGetLastError();
 }
 template <typename T> hipError_t grad_rows(const DistillRows& a, hipStream_t st) {
-  const int pieces = most_pieces(a, sizeof(T)), parts = parts_of(a.rows, pieces), share = (pieces + parts - 1) / parts;
+  const int pieces = most_pieces(a, sizeof(T)), parts = grad_parts(a.rows, pieces), share = (pieces + parts - 1) / parts;
   if (share <= 256) return grad_kernel<T, 64, 4>(a, parts, share, st);
   if (share <= 512) return grad_kernel<T, 128, 4>(a, parts, share, st);
   if (share <= 1024) return grad_kernel<T, 256, 4>(a, parts, share, st);
@@ -484,8 +491,8 @@ template <typename T> hipError_t grad_rows(const DistillRows& a, hipStream_t st)
   return grad_kernel<T, 1024, 16>(a, parts, share, st);
 }
 
-template <typename T, int THREADS, int R, int Q, int WAVES> hipError_t step_kernel(const DistillRows& a, hipStream_t st) {
-  const auto kernel = distill_step_kernel<T, THREADS, R, Q, WAVES>;
+template <typename T, int THREADS, int R, int Q, int WAVES, bool EVEN = true> hipError_t step_kernel(const DistillRows& a, hipStream_t st) {
+  const auto kernel = distill_step_kernel<T, THREADS, R, Q, WAVES, EVEN>;
   if constexpr (Q > 0) {
     static DeviceOnce once;
     const hipError_t e = once.run([&] { return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, Q * THREADS * 16 + 24 * 1024); });
@@ -496,13 +503,14 @@ template <typename T, int THREADS, int R, int Q, int WAVES> hipError_t step_kern
 }
 
 template <typename T> hipError_t step_rows(const DistillRows& a, void* ws, hipStream_t st) {
-  const int pieces = most_pieces(a, sizeof(T)), parts = parts_of(a.rows, pieces);
-  if (parts > 1 || !rows_even(a, sizeof(T))) {                // one after the other, with the stats behind the parts'
+  const int pieces = most_pieces(a, sizeof(T)), parts = step_parts(a.rows, pieces);
+  if (parts > 1) {                                            // one after the other, with the stats behind the parts'
     DistillRows b = a;
-    b.stats = (float*)ws + (parts > 1 ? 2 * (size_t)a.rows * parts : 0);
-    const hipError_t e = loss_rows<T>(b, ws, st);
+    b.stats = (float*)ws + 2 * (size_t)a.rows * parts;
+    const hipError_t e = loss_rows<T>(b, parts, ws, st);
     return e != hipSuccess ? e : grad_rows<T>(b, st);
   }
+  if (!rows_even(a, sizeof(T))) return step_kernel<T, 512, 16, 0, 4, false>(a, st);
   if (pieces <= 256) return step_kernel<T, 64, 4, 0, 4>(a, st);
   if (pieces <= 512) return step_kernel<T, 128, 4, 0, 4>(a, st);
   if (pieces <= 1024) return step_kernel<T, 256, 4, 0, 4>(a, st);
@@ -518,9 +526,10 @@ template <typename T> hipError_t step_rows(const DistillRows& a, void* ws, hipSt
 size_t distill_workspace(int rows, int vocab) {
   DistillRows a = {};
   a.vocab = vocab;
-  const int parts = parts_of(rows, most_pieces(a, 4));        // no fewer than of bf16 rows
-  return ((size_t)rows * ((parts > 1 ? parts : 0) + 1) * 2 * sizeof(float) + 255) / 256 * 256;
+  const int parts = step_parts(rows, most_pieces(a, 4));      // no fewer than of bf16 rows, or of a loss
+  return parts > 1 ? ((size_t)rows * (parts + 1) * 2 * sizeof(float) + 255) / 256 * 256 : 0;
 }
-hipError_t launch_distill(const DistillRows& a, bool bf16, void* ws, hipStream_t st) { return bf16 ? loss_rows<bf16_t>(a, ws, st) : loss_rows<float>(a, ws, st); }
+template <typename T> static hipError_t loss_as(const DistillRows& a, void* ws, hipStream_t st) { return loss_rows<T>(a, loss_parts(a.rows, most_pieces(a, sizeof(T))), ws, st); }
+hipError_t launch_distill(const DistillRows& a, bool bf16, void* ws, hipStream_t st) { return bf16 ? loss_as<bf16_t>(a, ws, st) : loss_as<float>(a, ws, st); }
 hipError_t launch_distill_grad(const DistillRows& a, bool bf16, hipStream_t st) { return bf16 ? grad_rows<bf16_t>(a, st) : grad_rows<float>(a, st); }
 hipError_t launch_distill_step(const DistillRows& a, bool bf16, void* ws, hipStream_t st) { return bf16 ? step_rows<bf16_t>(a, ws, st) : step_rows<float>(a, ws, st); }
