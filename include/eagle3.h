@@ -387,7 +387,7 @@ int eagle3_embed(int32_t dtype, int32_t rows, int32_t dim, int32_t vocab, const 
  * `accumulate` it is added to what d_table holds, and rows of other tokens are not touched (nor read).  The sum of a token's rows is formed in an
  * order that the tokens alone decide.
  *   dtype, out_dtype  of dy [rows, dim] and of d_table [vocab, dim] (dense)
- * Requires 1 <= rows < 2^22, 1 <= dim <= 65536, 1 <= vocab < 2^27. */
+ * Requires 1 <= rows < 2^22, 1 <= dim <= 65536, 1 <= vocab < 2^27, rows * dim < 2^36, vocab * dim < 2^33. */
 int eagle3_embed_grad(int32_t dtype, int32_t rows, int32_t dim, int32_t vocab, const void* dy, int64_t dy_stride, const int32_t* tokens, float scale,
                       int32_t accumulate, int32_t out_dtype, void* d_table, void* workspace, size_t workspace_bytes, eagle3_stream stream);
 int eagle3_embed_grad_workspace(int32_t rows, int32_t dim, int32_t vocab, size_t* bytes);
@@ -397,7 +397,7 @@ int eagle3_embed_grad_workspace(int32_t rows, int32_t dim, int32_t vocab, size_t
  *   residual, sum_out     [rows, dim] of sum_dtype, EAGLE3_FP32 or x_dtype; sum_out gets h and may be residual itself with the same stride.  Both NULL: no sum
  *   gain, gain_dtype      [dim]
  *   out, out_dtype        [rows, dim]; may be x itself with the same type and stride
- * Requires 1 <= rows < 2^24, 1 <= dim <= 16384, eps >= 0. */
+ * Requires 1 <= rows < 2^24, 1 <= dim <= 16384, eps >= 0.  Squares are summed in 32 bits: a row whose sum of squares passes 3.4e38 has a norm of zeros. */
 int eagle3_add_norm(int32_t rows, int32_t dim, int32_t x_dtype, const void* x, int64_t x_stride, int32_t sum_dtype, const void* residual,
                     int64_t residual_stride, void* sum_out, int64_t sum_stride, int32_t gain_dtype, const void* gain, float eps, int32_t out_dtype,
                     void* out, int64_t out_stride, eagle3_stream stream);
@@ -434,7 +434,7 @@ typedef struct {
   const float* lse;         /* DEVICE fp32 [rows]: log of the sum of exp(z / T) over the teacher's whole vocabulary, or NULL */
   const int32_t* t2d;       /* DEVICE [n_t2d]: the student's id of a teacher's token, negative: none; or NULL  */
   int32_t n_t2d, k;         /* 1 <= k <= 1024                                                                  */
-  float temperature;        /* T > 0, of the teacher and of the student                                        */
+  float temperature;        /* T, of the teacher and of the student: finite, at least 2^-126                   */
 } eagle3_teacher;
 
 /* Distillation: loss[r] = - sum_j p_j log softmax(logits[r] / T)[id_j], and its gradient d_logits[r][v] = dloss[r] / T (P softmax(logits[r] / T)[v] - p_v) with

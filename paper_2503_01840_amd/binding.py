@@ -715,9 +715,12 @@ def _recorded(*tensors):
 
 
 def _not_over_records(out, *inputs):
-    """Results go to new tensors where gradients are recorded."""
-    if _recorded(*inputs, *(out if isinstance(out, (tuple, list)) else (out,))):
+    """Results go to new tensors where gradients are recorded, and a backward pass is told what was written over since."""
+    outs = [t for t in (out if isinstance(out, (tuple, list)) else (out,)) if t is not None]
+    if _recorded(*inputs, *outs):
         _refuse("out", "None where gradients are recorded", out)
+    for t in outs:
+        torch.autograd.graph.increment_version(t)
 
 
 def _embed(table, tokens, scale, dtype, out):

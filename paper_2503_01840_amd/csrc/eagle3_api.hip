@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -909,7 +910,7 @@ int eagle3_embed(int32_t dtype, int32_t rows, int32_t dim, int32_t vocab, const 
 
 static int embed_grad_sizes(int32_t rows, int32_t dim, int32_t vocab) {
   if (rows < 1 || rows >= 1 << 22 || dim < 1 || dim > 65536 || (int64_t)rows * dim >= (int64_t)1 << 36 || vocab < 1 || vocab >= 1 << 27) return EAGLE3_E_SHAPE;
-  return EAGLE3_OK;
+  return (int64_t)vocab * dim >= (int64_t)1 << 33 ? EAGLE3_E_SHAPE : EAGLE3_OK;      // 2^31 threads write a table's zeros
 }
 
 int eagle3_embed_grad_workspace(int32_t rows, int32_t dim, int32_t vocab, size_t* bytes) {
@@ -998,7 +999,7 @@ static int distill_sizes(int32_t rows, int32_t vocab) { return rows < 1 || rows 
 
 static int distill_rows(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t stride, const eagle3_teacher* t, DistillRows& a) {
   if (!logits || !t || !t->ids || !t->values) return EAGLE3_E_NULL;
-  if (!real_type(dtype) || t->k < 1 || t->k > 1024 || (t->t2d && t->n_t2d < 1) || !(t->temperature > 0.f) || !std::isfinite(t->temperature)) return EAGLE3_E_SHAPE;
+  if (!real_type(dtype) || t->k < 1 || t->k > 1024 || (t->t2d && t->n_t2d < 1) || !(t->temperature >= FLT_MIN) || !std::isfinite(t->temperature)) return EAGLE3_E_SHAPE;
   TRY(distill_sizes(rows, vocab));
   if (!rows_fit(logits, stride, vocab, size_of(dtype))) return EAGLE3_E_SHAPE;
   a = {logits, stride, rows, vocab, t->ids, t->values, t->lse, t->t2d, t->n_t2d, t->k, t->temperature, nullptr, nullptr, nullptr, nullptr, 0, 64};

@@ -236,7 +236,7 @@ __global__ __launch_bounds__(1024) void add_norm_grad_kernel(NormGradRows b, int
         gh += red[turn][1][(wave & -W) + i];
       }
     }
-    const float r = 1.f / sqrtf(hh / (float)a.dim + a.eps), c = r * r * r * (gh / (float)a.dim);
+    const float r = 1.f / sqrtf(hh / (float)a.dim + a.eps), c = r * (gh / (float)a.dim);       // of the normalised row: r's cube leaves fp32 where a row is small
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       const int p = t + (j << lg);
@@ -244,10 +244,10 @@ __global__ __launch_bounds__(1024) void add_norm_grad_kernel(NormGradRows b, int
         float y[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const float d = dy[j].at(i), v = h[j].at(i);
-          y[i] = fmaf(g[j][i] * d, r, -(v * c));
+          const float d = dy[j].at(i), v = h[j].at(i) * r;
+          y[i] = r * fmaf(-v, c, g[j][i] * d);
           if (b.dh) y[i] += dh[j].at(i);
-          dg[j][i] = fmaf(d, v * r, dg[j][i]);
+          dg[j][i] = fmaf(d, v, dg[j][i]);
         }
         if (b.d_sum) store_piece<N, ODD>((H*)b.d_sum + row * b.d_sum_stride + (long long)p * N, y, a.dim - p * N);
         if (b.dx) store_piece<N, ODD>((X*)b.dx + row * b.dx_stride + (long long)p * N, y, a.dim - p * N);

@@ -43,7 +43,7 @@ EMBED_GRAD = dict(dtype=1, rows=200, dim=64, vocab=10, dy=AT, stride=64, tokens=
 
 @pytest.mark.parametrize("over,code", [(dict(dy=None), -1), (dict(tokens=None), -1), (dict(d_table=None), -1), (dict(dtype=2), -2), (dict(out_dtype=3), -2), (dict(rows=0), -2),
                                        (dict(rows=1 << 22), -2), (dict(dim=0), -2), (dict(dim=65537, stride=1 << 20), -2), (dict(rows=1 << 21, dim=1 << 15, stride=1 << 15), -2),
-                                       (dict(vocab=0), -2), (dict(vocab=1 << 27), -2), (dict(stride=63), -2), (dict(dy=AT + 1), -2), (dict(d_table=AT + 2), -2),
+                                       (dict(vocab=0), -2), (dict(vocab=1 << 27), -2), (dict(vocab=1 << 26, dim=128, stride=128), -2), (dict(stride=63), -2), (dict(dy=AT + 1), -2), (dict(d_table=AT + 2), -2),
                                        (dict(ws=None), -3), (dict(ws=AT + 128), -3), (dict(size=1000), -3)])
 def test_gradients_of_embeddings(L, over, code):
     assert L.eagle3_embed_grad(*_args(EMBED_GRAD, over)) == code
@@ -99,7 +99,7 @@ CALLS = {"eagle3_distill": {**HEAD, "loss": AT, "stats": None, "ws": AT, "size":
 def test_distillation(L, call):
     f = getattr(L, call)
     for over, code in [(dict(ids=None), -1), (dict(values=None), -1), (dict(k=0), -2), (dict(k=1025), -2), (dict(t2d=AT), -2), (dict(temperature=0.0), -2), (dict(temperature=-1.0), -2),
-                       (dict(temperature=math.inf), -2), (dict(temperature=math.nan), -2)]:
+                       (dict(temperature=math.inf), -2), (dict(temperature=math.nan), -2), (dict(temperature=1e-39), -2)]:
         assert f(*_args(CALLS[call], dict(teacher=_teacher(**over)))) == code, over
     wrong = [(dict(teacher=None), -1), (dict(logits=None), -1), (dict(dtype=2), -2), (dict(rows=0), -2), (dict(rows=1 << 24), -2), (dict(vocab=0), -2),
              (dict(vocab=1 << 27, stride=1 << 27), -2), (dict(stride=999), -2), (dict(stride=1 << 40), -2), (dict(logits=AT + 1), -2), (dict(loss=None), -1), (dict(dloss=None), -1), (dict(out=None), -1),
@@ -179,3 +179,24 @@ def test_what_tensors_have_to_be(sent):
     assert sent[-1][4] == 40 and sent[-1][7] == 20
     E.eagle3_distill_step(z(1), z(9, 50)[::9, :16], i(1, 3), z(1, 3))
     assert sent[-1][4] == 16
+
+
+def test_what_is_written_over_is_known_to_a_backward_pass(sent):
+    """A result written over what a recorded call keeps for its gradient: the backward pass says so."""
+    ids, values = torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2)
+    logits = torch.zeros(4, 16).requires_grad_()
+    loss = E.eagle3_distill(logits, ids, values).sum()
+    E.eagle3_distill_step(torch.ones(4), logits.detach(), ids, values, out=logits.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    gain = torch.ones(16).requires_grad_()
+    y, h = E.eagle3_add_norm(torch.zeros(4, 16), gain, 1e-5, residual=torch.zeros(4, 16))
+    E.eagle3_add_norm(torch.zeros(4, 16), gain.detach(), 1e-5, residual=h.detach(), out=(None, h.detach()))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    x, at = torch.zeros(4, 16), torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: E.eagle3_embed(x, at, out=x), lambda: E.eagle3_embed_grad(x, at, 4, out=x), lambda: E.eagle3_add_norm(x, x[0], 1e-5, out=x),
+                 lambda: E.eagle3_add_norm_codes(x, x[0], 1e-5, residual=x, out=x), lambda: E.eagle3_distill_grad(x[:, 0].contiguous(), torch.zeros(4, 2), x, ids, values, out=x)):
+        before = x._version
+        call()
+        assert x._version == before + 1

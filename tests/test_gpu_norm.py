@@ -224,6 +224,18 @@ def test_infinities_stay_in_their_row():
     assert bool(dx[3].isnan().all())
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -50, 2.0 ** -20, 2.0 ** 50])
+def test_small_and_large_rows(scale):
+    """Rows of any magnitude whose squares fp32 holds: the norm is the same, the gradient 1 / scale of it (a power of two: bit for bit, with eps = 0)."""
+    g = torch.Generator().manual_seed(5)
+    h, dy, gain = (torch.randn(*s, generator=g).to(DEV) for s in ((70, 500), (70, 500), (500,)))
+    y, (dx, d_sum, d_gain) = E.eagle3_add_norm(h, gain, 0.0), E.eagle3_add_norm_grad(dy, h, gain, 0.0)
+    assert torch.equal(E.eagle3_add_norm(h * scale, gain, 0.0), y)
+    got = E.eagle3_add_norm_grad(dy, h * scale, gain, 0.0)
+    assert torch.equal(got[0], dx / scale) and torch.equal(got[1], d_sum / scale) and torch.equal(got[2], d_gain)
+    assert bool(dx.isfinite().all()) and float(dx.abs().max()) > 0
+
+
 def test_captured_norms_replay():
     g = torch.Generator().manual_seed(5)
     x, res, dy = (torch.zeros(900, 264, device=DEV) for _ in range(3))
