@@ -6,7 +6,7 @@
 // 32000 in fp32 163 us instead of 107, 2047 of 128256 in bf16 312 instead of 223).  The teacher's weights are one wavefront's work while the row is on its way;
 // the gradient's entries of its tokens are written a second time, once the row is written.  A token's weights go to its first entry, found by a hash (by comparing
 // all entries 345 us instead of 233, with 128 of them), in the order of entries: results do not change from call to call.
-// Bound by bytes, the logits read, the gradient written, at 4.5 to 5.2 TB/s where rows are many; in bf16 the exponentials take half of that time under the loads.
+// Bound by bytes, the logits read, the gradient written, at 4.3 to 5.2 TB/s where rows are many; in bf16 the exponentials take half of that time under the loads.
 #include <algorithm>
 
 #include "elements.hpp"
@@ -458,11 +458,11 @@ template <typename T> hipError_t loss_rows(const DistillRows& a, int parts, void
   if (parts > 1) {
     hipLaunchKernelGGL((distill_part_kernel<T, 256>), grid_of(a.rows, parts), dim3(256), 0, st, a, factor_of(a), (pieces + parts - 1) / parts, (float*)ws);
     loss_kernel<T, 64>(a, (const float*)ws, parts, st);
-  } else if (pieces <= 256) {
-    loss_kernel<T, 64>(a, nullptr, 0, st);
-  } else if (pieces <= 512) {
-    loss_kernel<T, 128>(a, nullptr, 0, st);
-  } else if (pieces <= 2048) {
+  } else if (pieces <= 512) {                                 // eight pieces to a thread: fewer take longer where rows are many, and no less where they are few
+    loss_kernel<T, 64>(a, nullptr, 0, st);                    // 16384 bf16 rows of 4000 29 us, with 128 threads 40 (64 rows 5.0, 5.0)
+  } else if (pieces <= 1024) {
+    loss_kernel<T, 128>(a, nullptr, 0, st);                   // 8192 of 8000 28, with 256 37 (64 rows 5.1, 5.0)
+  } else if (pieces <= 2048) {                                // 3000 of 16000 19.9, with 128 20.6, with 512 26.5
     loss_kernel<T, 256>(a, nullptr, 0, st);
   } else {
     loss_kernel<T, 512>(a, nullptr, 0, st);
@@ -481,6 +481,8 @@ template <typename T, int THREADS, int R> hipError_t grad_kernel(const DistillRo
     hipLaunchKernelGGL((distill_grad_kernel<T, THREADS, R, false>), grid_of(a.rows, parts), dim3(THREADS), lds_of(a), st, a, factor_of(a), share);
   return hipGetLastError();
 }
+// Threads and pieces that each asks for ahead.  us, many rows: 500 pieces 128 x 4 51.8 (64 x 4 61.5, 256 x 4 59.3), 1000 256 x 4 53.2 (128 x 4 56.9, 256 x 16 57.1), 2000 256 x 16 55.7
+// (256 x 4 60.7, 512 x 16 65.6), 4000 512 x 16 104.3 (256 x 16 108.6), 16000 1024 x 16 203.2 (512 x 16 204.4).
 template <typename T> hipError_t grad_rows(const DistillRows& a, hipStream_t st) {
   const int pieces = most_pieces(a, sizeof(T)), parts = grad_parts(a.rows, pieces), share = (pieces + parts - 1) / parts;
   if (share <= 256) return grad_kernel<T, 64, 4>(a, parts, share, st);
@@ -502,6 +504,8 @@ template <typename T, int THREADS, int R, int Q, int WAVES, bool EVEN = true> hi
   return hipGetLastError();
 }
 
+// The fewest threads whose registers hold a row.  us, many rows: 500 pieces 128 x 4 53.9 (64 x 4, half of the row read twice, 64.7; 256 x 4 65.5), 1000 256 x 4 54.2 (256 x 8 57.5),
+// 2000 256 x 8 55.8 (512 x 8 64.4), 4000 512 x 8 103.5 (512 x 16 105.1, 1024 x 16 202), 8000 512 x 16 106 (1024 x 16 140), 31250 1024 x 16 and 8 in LDS 115 (without these 133).
 template <typename T> hipError_t step_rows(const DistillRows& a, void* ws, hipStream_t st) {
   const int pieces = most_pieces(a, sizeof(T)), parts = step_parts(a.rows, pieces);
   if (parts > 1) {                                            // one after the other, with the stats behind the parts'

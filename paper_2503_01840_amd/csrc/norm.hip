@@ -2,7 +2,7 @@
 //
 // A row h = x + residual is read once into the registers of its 8 to 1024 threads, its squares are summed by exchanges within the wavefronts and through LDS between
 // them, and the row is written as h and as gain * h / sqrt(mean + eps).  The gradient's rows go to at most 512 workgroups in turn, which keep the gains' gradient in
-// registers; their parts are added by a second launch (4 us).  Bound by bytes, at a large copy's rate and above where rows are many: 16384 rows of 8192 in bf16 178 us
+// registers; their parts are added by a second launch (4.8 us).  Bound by bytes, at a large copy's rate and above where rows are many: 16384 rows of 8192 in bf16 178 us
 // (6.0 TB/s), 8192 of 4096 onto an fp32 stream 72 (5.6), 2048 of 8192 in 8 bits 24 (4.9), the gradient of 8191 rows of 4096 on an fp32 stream 102 (5.3).
 // Measured and not kept: an eighth of the rows to each XCD (2 to 17 % slower); the gradient's next row asked for while one is worked on (0 to 8 % slower); results stored past the
 // caches (2 to 10 % faster alone, but with an addition behind it that reads them 4096 rows of 8192 in bf16 72 -> 79 us).
@@ -347,7 +347,8 @@ int type_size(int t) { return t == NORM_FP32 ? 4 : t == NORM_BF16 ? 2 : 1; }
 template <typename X, typename H, typename Y, bool ODD, int P>
 hipError_t launch_backward(const NormGradRows& b, int lg, hipStream_t st) {
   const int threads = std::max(256, 1 << lg), per = threads >> lg;
-  const int grid = std::min((b.fwd.rows + per - 1) / per, NORM_GRAD_PARTS);
+  // one round of workgroups leaves as many parts as there are rows: two rows to each then.  512 bf16 rows of 8192 20.0 us in 512 parts, 15.7 in 256, 17.9 in 128; 1024 rows 21.1, 22.1, 26.3
+  const int blocks = (b.fwd.rows + per - 1) / per, grid = std::min(blocks, blocks <= NORM_GRAD_PARTS ? NORM_GRAD_PARTS / 2 : NORM_GRAD_PARTS);
   hipLaunchKernelGGL((add_norm_grad_kernel<X, H, Y, ODD, P>), dim3(grid), dim3(threads), per > 1 ? padded(b.fwd.dim) * sizeof(float) : 0, st, b, lg);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !b.partial) return e;
