@@ -675,9 +675,14 @@ def _like(t, n, d, gpu, what, dtype=None):
 def _vector(t, d, gpu, what):
     """(address, type) of a dense [d] in bf16 or fp32."""
     code = _TYPES.get(t.dtype)
-    if code is None:
-        _refuse(what, "bf16 or fp32", t)
-    return _arg(t, t.dtype, (d,), gpu, what), code
+    if code is None or t.get_device() != gpu or t.shape != (d,) or not t.is_contiguous():
+        _refuse(what, f"a dense bf16 or fp32 tensor [{d}] on cuda:{gpu}", t)
+    return t.data_ptr(), code
+
+
+def _dense_like(t):
+    """A dense tensor of this type and shape (half a microsecond sooner where t is dense, as it mostly is)."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _type(dtype, what):
@@ -808,7 +813,7 @@ def _sum_out(h, residual, n, d, gpu):
             _refuse("out of the sum", "None without residual", h)
         return None, None, d
     if h is None:
-        h = torch.empty_like(residual, memory_format=torch.contiguous_format)
+        h = _dense_like(residual)
         return h, h.data_ptr(), d
     hp, _, _, hs, _ = _like(h, n, d, gpu, "out of the sum", residual.dtype)
     return h, hp, hs
@@ -819,7 +824,7 @@ def _add_norm(x, gain, eps, residual, dtype, out):
     y, h = out if isinstance(out, (tuple, list)) else (out, None)
     h, hp, hs = _sum_out(h, residual, n, d, gpu)
     if y is None:
-        y = x.new_empty((n, d), dtype=dtype)
+        y = _dense_like(x) if dtype is None else x.new_empty((n, d), dtype=dtype)
         yp, ys, yc = y.data_ptr(), d, xa[2] if dtype is None else _TYPES[dtype]
     else:
         yp, _, _, ys, yc = _like(y, n, d, gpu, "out", dtype)
@@ -882,7 +887,7 @@ def _add_norm_grad(dy, h, gain, eps, dh, x_dtype, want_gain):
     xc = _type(x_dtype, "x_dtype")
     if hc != EAGLE3_FP32 and hc != xc:
         _refuse("x_dtype", f"that of h ({h.dtype})", x_dtype)
-    d_sum = torch.empty_like(h, memory_format=torch.contiguous_format)
+    d_sum = _dense_like(h)
     dx = d_sum if xc == hc else h.new_empty((n, d), dtype=x_dtype)
     d_gain = torch.empty_like(gain) if want_gain else None
     ws, size, _keep = _workspace("eagle3_add_norm_grad_workspace", (n, d), h) if want_gain else (None, 0, None)
@@ -947,7 +952,7 @@ def eagle3_distill(logits, ids, values, lse=None, t2d=None, temperature=1.0, wan
 
 def _gradient_out(out, logits, n, V, gpu):
     if out is None:
-        out = logits.new_empty((n, V))
+        out = _dense_like(logits)
         return out, out.data_ptr(), V
     _not_over_records(out)
     op, _, _, stride, _ = _like(out, n, V, gpu, "out", logits.dtype)

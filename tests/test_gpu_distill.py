@@ -41,8 +41,9 @@ def _reference(logits, ids, values, lse, t2d, T, dloss):
     dense = torch.zeros_like(x).scatter_add_(1, at, p)
     g = (dloss.double().cpu() / T)[:, None]
     grad = g * (P * logq.exp() - dense)
-    # Sum: exponents off by 3 U of their size (difference, factor, product) and the exponential by 2 U; a thread rescales its sum once a batch of at least 2048 elements of
-    # the row, between threads 6 + 15 times, each by as much; additions of a batch's 32 and of 22 sums.  Weights: exponents off by 2 U of theirs, the exponential 2 U, a sum of
+    # Sum: exponents off by 3 U of their size (difference, factor, product) and the exponential by 2 U; a thread rescales its sum once for 16 values, 8 times
+    # in a row that registers hold and V / 8192 times in a longer one, between threads 6 + 15 times, each by 3 U more; it adds up to V / 1024 values in a chain, 32 where V is below
+    # 16384, and 22 sums: 3 (8 + 21) + 32 + 22 or 3 (8 + V / 8192 + 21) + V / 1024 + 22 steps, less than 4 (V / 2048 + 22) + 60 at every V.  Weights: exponents off by 2 U of theirs, the exponential 2 U, a sum of
     # k terms, a quotient.
     spread = (m - x.amin(1, keepdim=True)).clamp(max=104)     # what is further below has no part in the sum
     rel_s = (3 * spread + 4 * (V / 2048 + 22) + 60) * U

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2503_01840_amd as E
+from every import every
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -41,12 +42,11 @@ def _strided(x, how):
     return view, wide
 
 
-SIZES = [(1, 1, 1), (1, 4096, 128256), (3, 8, 7), (64, 250, 2048), (65, 1001, 300), (1000, 256, 50), (2, 65536, 5), (9, 12000, 33), (60, 4096, 1000)]
+SIZES = [(1, 1, 1), (1, 4096, 20000), (3, 8, 7), (64, 250, 2048), (65, 1001, 300), (1000, 256, 50), (2, 65536, 5), (9, 12000, 33), (60, 4096, 1000)]
 
 
-@pytest.mark.parametrize("how", ["dense", "apart", "off"])
-@pytest.mark.parametrize("types", [(BF16, BF16), (BF16, FP32), (FP32, FP32), (FP32, BF16)])
 @pytest.mark.parametrize("rows,dim,vocab", SIZES)
+@every(types=[(BF16, BF16), (BF16, FP32), (FP32, FP32), (FP32, BF16)], how=["dense", "apart", "off"])
 def test_rows_of_the_table(rows, dim, vocab, types, how):
     g = torch.Generator().manual_seed(rows + dim)
     table = torch.randn(vocab, dim, generator=g).to(types[0]).to(DEV)
@@ -82,13 +82,12 @@ def _check_grad(got, dy, tok, vocab, scale, old=None):
     assert bool(((got.double().cpu() - want).abs() <= bound).all())
 
 
-GRADS = [(1, 1, 1), (1, 8, 5), (31, 64, 9), (32, 520, 40), (33, 251, 40), (64, 8, 2), (100, 264, 128256), (1000, 130, 2048), (4096, 40, 511), (4096, 16, 512), (4097, 72, 513),
+GRADS = [(1, 1, 1), (1, 8, 5), (31, 64, 9), (32, 520, 40), (33, 251, 40), (64, 8, 2), (100, 264, 30000), (1000, 130, 2048), (4096, 40, 511), (4096, 16, 512), (4097, 72, 513),
          (9000, 24, 128256), (20000, 8, 300000), (12289, 5, 131071)]
 
 
-@pytest.mark.parametrize("how", ["any", "same", "few", "ends", "padding"])
-@pytest.mark.parametrize("types", [(BF16, BF16), (BF16, FP32), (FP32, FP32), (FP32, BF16)])
 @pytest.mark.parametrize("rows,dim,vocab", GRADS)
+@every(types=[(BF16, BF16), (BF16, FP32), (FP32, FP32), (FP32, BF16)], how=["any", "same", "few", "ends", "padding"])
 def test_gradient_of_the_table(rows, dim, vocab, types, how):
     g = torch.Generator().manual_seed(rows + vocab)
     tok = _tokens(g, rows, vocab, how).to(DEV)

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2503_01840_amd as E
+from every import every
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -41,9 +42,8 @@ TYPES = [(BF16, BF16, BF16), (BF16, FP32, BF16), (FP32, FP32, FP32), (FP32, FP32
 SIZES = [(1, 1), (1, 8192), (3, 64), (5, 127), (4, 4096), (60, 250), (1025, 72), (1030, 1000), (2, 16384), (2, 16383), (1100, 2056), (7, 4104), (1024, 8192)]
 
 
-@pytest.mark.parametrize("how", ["dense", "apart", "off"])
-@pytest.mark.parametrize("types", TYPES)
 @pytest.mark.parametrize("rows,dim", SIZES)
+@every(types=TYPES, how=["dense", "apart", "off"])
 def test_norm_and_sum(rows, dim, types, how):
     xt, ht, yt = types
     g = torch.Generator().manual_seed(rows + dim)
@@ -72,9 +72,8 @@ def test_norm_and_sum(rows, dim, types, how):
             assert bool((around[:, :off] == 5).all()) and bool((around[:, off + dim:] == 5).all())
 
 
-@pytest.mark.parametrize("group", [0, 128])
-@pytest.mark.parametrize("types", [(BF16, BF16), (BF16, FP32), (FP32, FP32)])
 @pytest.mark.parametrize("rows,dim", [(1, 1), (1, 8192), (3, 64), (5, 127), (4, 4096), (60, 250), (1025, 72), (1030, 1000), (2, 16384), (2, 16383), (33, 129), (1100, 2056), (9, 136)])
+@every(types=[(BF16, BF16), (BF16, FP32), (FP32, FP32)], group=[0, 128])
 def test_norm_in_8_bits(rows, dim, types, group):
     xt, ht = types
     g = torch.Generator().manual_seed(rows + dim)
@@ -136,9 +135,8 @@ def _gradient(dy, h, gain, dh, eps=EPS):
     return d, (dy * h * r).sum(0), mag, (dy * h * r).abs().sum(0)
 
 
-@pytest.mark.parametrize("how", ["dense", "apart", "off"])
-@pytest.mark.parametrize("types", TYPES)
-@pytest.mark.parametrize("rows,dim", SIZES + [(513, 16), (2050, 13), (40, 6001)])
+@pytest.mark.parametrize("rows,dim", SIZES + [(513, 16), (2050, 13), (40, 6001), (300, 2050)])
+@every(types=TYPES, how=["dense", "apart", "off"])
 def test_gradient(rows, dim, types, how):
     xt, ht, yt = types
     g = torch.Generator().manual_seed(rows + dim)
