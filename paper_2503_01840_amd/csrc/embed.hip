@@ -6,7 +6,7 @@
 // Gradient: the rows' tokens are sorted first, so that a token's rows are neighbours and their sum has an order of its own: up to 12288 rows by counting smaller ones in one launch, beyond by
 // digits of at most 9 bits in two launches each.  Workgroups behind those that sort write zeros to the table meanwhile.  Then CHUNK sorted places at a time are summed by a wavefront for 64
 // pieces of columns, all CHUNK rows on their way at once; a token's sum that lies within them is written at once, the ends of one that does not go to the workspace and are added by the
-// last launch.  Bound by bytes, of which a large table's zeros are nearly all: 8192 rows of 4096 into 128256 in bf16 158 us for tokens and zeros (1051 MB, 6.7 TB/s), 17 and 6 for the sums;
+// last launch; few rows are summed in one launch, token by token.  Bound by bytes, of which a large table's zeros are nearly all: 8192 rows of 4096 into 128256 in bf16 158 us for tokens and zeros (1051 MB, 6.7 TB/s), 17 and 6 for the sums;
 // 1021 fp32 rows of 251 into 2048 6.2, 7.6 and 3.1, three launches that wait for memory.
 // Measured and not kept: one launch without sorted tokens for up to 1024 rows, each workgroup looking through all tokens for its part of the table (1021 rows of 251: 16.8 -> 15.4 us, but
 // 33 where half of the rows have one token, 61 where all have; tables of 1 GB 168 -> 171); zeros by the launch that sums; a token's rows 8 or 32 at a time.
@@ -362,6 +362,92 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restri
   store_piece<N, ODD>(to, f, dim - p * N);
 }
 
+// Few rows: no parts and no second launch.  A workgroup has the tokens whose first place is one of CHUNK, a wavefront each; one with more than 64 rows, the last, is summed by all wavefronts, a
+// 16th of its places each.  With one token in many rows a CU draws them alone, so this is for few: us, sums and parts in two launches against this, tokens of a log-uniform rank and one token
+// in all rows: 300 rows of 4096 20.4 and 16.3, 19.9 and 19.3; 400 20.5 and 17.2, 20.4 and 21.0; 512 20.6 and 17.2, 21.2 and 26.8; 2048 25.5 and 28.2, 32.1 and 66.9.
+constexpr int RUN_ROWS = 384;
+template <typename T, typename O, bool ODD, bool ADD>
+__global__ __launch_bounds__(1024) void embed_runs_kernel(const int32_t* __restrict__ token, const int32_t* __restrict__ row_of, int n, int dim, int vocab, EmbedGrad g) {
+  constexpr int N = sizeof(T) + sizeof(O) == 4 ? 8 : 4, U = 16;
+  __shared__ float part[16][64 * N];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int first = blockIdx.x * CHUNK, p = blockIdx.y * 64 + lane, left = dim - p * N;
+  const bool has = p < pieces_of(dim, N);
+  const int before = first ? token[first - 1] : -1, mine = first + lane < n ? token[first + lane] : vocab;       // padding, and what is behind the end: vocab
+  const int row = first + lane < n ? row_of[first + lane] : 0;
+  const int previous = __shfl_up(mine, 1, 64);
+  const uint64_t ends = __ballot(mine != (lane ? previous : before));             // places where another token begins
+  const uint64_t starts = __ballot(mine < vocab) & ends & ((1ull << CHUNK) - 1);
+  if (!starts) return;
+  const T* dy = (const T*)g.dy + (size_t)p * N;
+  float sum[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum[i] = 0.f;
+  auto add_rows = [&](int rows, int from, int to) {           // of lanes from..to-1
+    for (int l = from; l < to; l += U) {
+      Piece<T, N> e[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+        if (l + j < to && has) e[j].template load<ODD>(dy + (size_t)__builtin_amdgcn_readlane(rows, l + j) * g.stride, left);
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (l + j < to) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) sum[i] += has ? e[j].at(i) : 0.f;
+        }
+      }
+    }
+  };
+  auto leave = [&](int v) {
+    if (!has) return;
+    O* to = (O*)g.d_table + (size_t)v * dim + (size_t)p * N;
+    float f[N];
+    Piece<O, N> old;
+    if constexpr (ADD) old.template load<ODD>(to, left);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = ADD ? fmaf(g.scale, sum[i], old.at(i)) : g.scale * sum[i];
+    store_piece<N, ODD>(to, f, left);
+  };
+  const int last = 63 - __builtin_clzll(starts);              // the last start: its token may go on behind these 64 places
+  const bool is_long = ends >> (last + 1) == 0;
+  uint64_t left_starts = starts;
+  for (int w = 0; w < wave && left_starts; ++w) left_starts &= left_starts - 1;
+  if (left_starts) {
+    const int at = __builtin_ctzll(left_starts);
+    if (at != last || !is_long) {
+      add_rows(row, at, at + 1 + __builtin_ctzll(ends >> (at + 1)));
+      leave(__builtin_amdgcn_readlane(mine, at));
+    }
+  }
+  if (!is_long) return;
+  const int v = __builtin_amdgcn_readlane(mine, last);
+  int length = 64 - last;
+  for (;;) {
+    const int i = first + last + length + lane;
+    const uint64_t same = __ballot(i < n && token[i] == v);
+    length += __popcll(same);
+    if (~same) break;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum[i] = 0.f;
+  const int from = first + last + (int)((long long)length * wave / 16), to = first + last + (int)((long long)length * (wave + 1) / 16);
+  for (int l = from; l < to; l += 64) {
+    const int rows = l + lane < to ? row_of[l + lane] : 0;
+    add_rows(rows, 0, min(64, to - l));
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) part[wave][lane * N + i] = sum[i];
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    sum[i] = part[0][lane * N + i];
+#pragma unroll
+    for (int w = 1; w < 16; ++w) sum[i] += part[w][lane * N + i];
+  }
+  leave(v);
+}
+
 // ---------------------------------------------------------------- the workspace: keys and rows, twice, counts, parts
 size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
 int chunks_of(int rows) { return (rows + CHUNK - 1) / CHUNK; }
@@ -404,10 +490,14 @@ hipError_t sums_of(EmbedGrad g, char* ws, hipStream_t st) {
   if (e != hipSuccess) return e;
   g.partial = (float*)(ws + 4 * aligned((size_t)g.rows * sizeof(int32_t)) + aligned((size_t)((g.rows + TILE - 1) / TILE) * DIGITS * sizeof(uint32_t)));
   constexpr int N = sizeof(T) + sizeof(O) == 4 ? 8 : 4;
+  if (g.rows <= RUN_ROWS) {
+    hipLaunchKernelGGL((embed_runs_kernel<T, O, ODD, ADD>), dim3(chunks_of(g.rows), (pieces_of(g.dim, N) + 63) / 64), dim3(1024), 0, st, token, row, g.rows, g.dim, g.vocab, g);
+    return hipGetLastError();
+  }
   const int slabs = (pieces_of(g.dim, N) + 63) / 64, sums = chunks_of(g.rows) * slabs;
   hipLaunchKernelGGL((embed_sum_kernel<T, O, ODD, ADD>), dim3((sums + 3) / 4), dim3(256), 0, st, token, row, g.rows, g.dim, g.vocab, slabs, sums, g);
   e = hipGetLastError();
-  if (e != hipSuccess || g.rows <= CHUNK) return e;
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL((embed_join_kernel<O, ODD, ADD>), dim3(chunks_of(g.rows), (g.dim + 255) / 256), dim3(256), 0, st, token, g.rows, g.dim, g.vocab, g);
   return hipGetLastError();
 }
@@ -434,7 +524,7 @@ hipError_t launch_embed(const EmbedRows& a, bool table_bf16, bool out_bf16, hipS
 
 size_t embed_grad_workspace(int rows, int dim) {
   return 4 * aligned((size_t)rows * sizeof(int32_t)) + aligned((size_t)((rows + TILE - 1) / TILE) * DIGITS * sizeof(uint32_t)) +
-         (rows > CHUNK ? aligned((size_t)chunks_of(rows) * 2 * padded(dim) * sizeof(float)) : 0);
+         (rows > RUN_ROWS ? aligned((size_t)chunks_of(rows) * 2 * padded(dim) * sizeof(float)) : 0);
 }
 
 hipError_t launch_embed_grad(const EmbedGrad& g, bool dy_bf16, bool out_bf16, bool add, void* ws, hipStream_t st) {

@@ -83,7 +83,7 @@ def _check_grad(got, dy, tok, vocab, scale, old=None):
 
 
 GRADS = [(1, 1, 1), (1, 8, 5), (31, 64, 9), (32, 520, 40), (33, 251, 40), (64, 8, 2), (100, 264, 30000), (1000, 130, 2048), (4096, 40, 511), (4096, 16, 512), (4097, 72, 513),
-         (9000, 24, 128256), (20000, 8, 300000), (12289, 5, 131071)]
+         (9000, 24, 128256), (20000, 8, 300000), (12289, 5, 131071), (17, 4104, 30), (80, 260, 3), (200, 1030, 7), (384, 72, 1000), (385, 72, 1000)]
 
 
 @pytest.mark.parametrize("rows,dim,vocab", GRADS)
