@@ -324,8 +324,9 @@ hipError_t forward(const NormRows& a, hipStream_t st) {
   constexpr int N = piece_size<X, H, Y>();
   const int pieces = pieces_of(a.dim, N), lg = threads_of(pieces, N == 8 && ADDED && sizeof(Y) > 1 && pieces >= 1024 ? 1 : 2, a.rows, sizeof(Y) > 1 ? 3 : N == 8 ? 4 : 5), P = (pieces + (1 << lg) - 1) >> lg;
   if (P <= 1) return launch_forward<X, H, Y, ADDED, ODD, 1>(a, lg, st);
-  if (P <= 2) return launch_forward<X, H, Y, ADDED, ODD, 2>(a, lg, st);
-  return launch_forward<X, H, Y, ADDED, ODD, 4>(a, lg, st);
+  if constexpr (N == 4)
+    if (P > 2) return launch_forward<X, H, Y, ADDED, ODD, 4>(a, lg, st);
+  return launch_forward<X, H, Y, ADDED, ODD, 2>(a, lg, st);                        // 2048 pieces of 8 at most
 }
 
 template <typename X, typename H, typename Y>
@@ -347,8 +348,9 @@ int type_size(int t) { return t == NORM_FP32 ? 4 : t == NORM_BF16 ? 2 : 1; }
 template <typename X, typename H, typename Y, bool ODD, int P>
 hipError_t launch_backward(const NormGradRows& b, int lg, hipStream_t st) {
   const int threads = std::max(256, 1 << lg), per = threads >> lg;
-  // one round of workgroups leaves as many parts as there are rows: two rows to each then.  512 bf16 rows of 8192 20.0 us in 512 parts, 15.7 in 256, 17.9 in 128; 1024 rows 21.1, 22.1, 26.3
-  const int blocks = (b.fwd.rows + per - 1) / per, grid = std::min(blocks, blocks <= NORM_GRAD_PARTS ? NORM_GRAD_PARTS / 2 : NORM_GRAD_PARTS);
+  // A workgroup to a CU where it has 1024 threads, else two; one also where a single round of them would leave as many parts as there are rows.  us in 512, 256, 128 parts: 512 bf16 rows
+  // of 8192 20.0, 15.7, 17.9; 1024 rows 21.1, 22.1, 26.3; 8191 rows of 4096 on an fp32 stream 102, 121, 215; 2048 of 16384 138, 128
+  const int blocks = (b.fwd.rows + per - 1) / per, grid = std::min(blocks, threads == 1024 || blocks <= NORM_GRAD_PARTS ? NORM_GRAD_PARTS / 2 : NORM_GRAD_PARTS);
   hipLaunchKernelGGL((add_norm_grad_kernel<X, H, Y, ODD, P>), dim3(grid), dim3(threads), per > 1 ? padded(b.fwd.dim) * sizeof(float) : 0, st, b, lg);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !b.partial) return e;
@@ -361,8 +363,9 @@ hipError_t backward(const NormGradRows& b, hipStream_t st) {
   constexpr int N = piece_size<X, H, Y>();
   const int pieces = pieces_of(b.fwd.dim, N), lg = threads_of(pieces, 2, b.fwd.rows, 3), P = (pieces + (1 << lg) - 1) >> lg;
   if (P <= 1) return launch_backward<X, H, Y, ODD, 1>(b, lg, st);
-  if (P <= 2) return launch_backward<X, H, Y, ODD, 2>(b, lg, st);
-  return launch_backward<X, H, Y, ODD, 4>(b, lg, st);
+  if constexpr (N == 4)
+    if (P > 2) return launch_backward<X, H, Y, ODD, 4>(b, lg, st);
+  return launch_backward<X, H, Y, ODD, 2>(b, lg, st);
 }
 
 template <typename X, typename H, typename Y>
