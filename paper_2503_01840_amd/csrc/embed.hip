@@ -36,13 +36,14 @@ __global__ __launch_bounds__(256) void embed_kernel(const int32_t* tokens, const
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int p = p0 + 64 * j + lane;
-      if (seen && p < last) e[j].template load<ODD>(from + (size_t)p * N, dim - p * N);
+      if (seen && p < last) e[j].template load<ODD>(from + (size_t)p * N, dim - p * N, dim);
     }
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int p = p0 + 64 * j + lane;
       if (p < last) {
         float f[N];
+        e[j].template settle<ODD>(dim - p * N, dim);
 #pragma unroll
         for (int i = 0; i < N; ++i) f[i] = seen ? scale * e[j].at(i) : 0.f;
         store_piece<N, ODD, STREAM>(to + (size_t)p * N, f, dim - p * N);
@@ -284,7 +285,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restric
     float f[N];
     if constexpr (ADD) {
       Piece<O, N> old;
-      old.template load<ODD>(to, left);
+      old.template load<ODD>(to, left, dim);
+      old.template settle<ODD>(left, dim);
 #pragma unroll
       for (int i = 0; i < N; ++i) f[i] = fmaf(g.scale, sum[i], old.at(i));
     } else {
@@ -296,7 +298,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restric
   Piece<T, N> e[CHUNK];
 #pragma unroll
   for (int j = 0; j < CHUNK; ++j)                             // places behind the last have row 0, which is not added
-    if (has) e[j].template load<ODD>(dy + (size_t)__builtin_amdgcn_readlane(rows, j) * g.stride, left);
+    if (has) e[j].template load<ODD>(dy + (size_t)__builtin_amdgcn_readlane(rows, j) * g.stride, left, dim);
 #pragma unroll
   for (int j = 0; j < CHUNK; ++j) {
     const int next = __builtin_amdgcn_readlane(tokens, j);
@@ -308,6 +310,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int32_t* __restric
 #pragma unroll
       for (int i = 0; i < N; ++i) sum[i] = 0.f;
     }
+    e[j].template settle<ODD>(left, dim);
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] += has ? e[j].at(i) : 0.f;
   }
@@ -341,7 +344,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restri
 #pragma unroll 4
     for (int c = wave * share; c < min(parts, (wave + 1) * share); ++c) {
       Piece<float, N> e;
-      e.template load<false>(g.partial + ((size_t)(chunk + c) * 2 + (c ? 0 : 1)) * padded(dim) + (size_t)p * N, N);
+      e.template load<false>(g.partial + ((size_t)(chunk + c) * 2 + (c ? 0 : 1)) * padded(dim) + (size_t)p * N, N, N);
 #pragma unroll
       for (int i = 0; i < N; ++i) sum[i] += e.at(i);
     }
@@ -353,7 +356,10 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restri
   float f[N];
   O* to = (O*)g.d_table + (size_t)v * dim + (size_t)p * N;
   Piece<O, N> old;
-  if constexpr (ADD) old.template load<ODD>(to, dim - p * N);
+  if constexpr (ADD) {
+    old.template load<ODD>(to, dim - p * N, dim);
+    old.template settle<ODD>(dim - p * N, dim);
+  }
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const float s = (part[0][lane * N + i] + part[1][lane * N + i]) + (part[2][lane * N + i] + part[3][lane * N + i]);
@@ -388,10 +394,11 @@ __global__ __launch_bounds__(1024) void embed_runs_kernel(const int32_t* __restr
       Piece<T, N> e[U];
 #pragma unroll
       for (int j = 0; j < U; ++j)
-        if (l + j < to && has) e[j].template load<ODD>(dy + (size_t)__builtin_amdgcn_readlane(rows, l + j) * g.stride, left);
+        if (l + j < to && has) e[j].template load<ODD>(dy + (size_t)__builtin_amdgcn_readlane(rows, l + j) * g.stride, left, dim);
 #pragma unroll
       for (int j = 0; j < U; ++j) {
         if (l + j < to) {
+          e[j].template settle<ODD>(left, dim);
 #pragma unroll
           for (int i = 0; i < N; ++i) sum[i] += has ? e[j].at(i) : 0.f;
         }
@@ -403,7 +410,10 @@ __global__ __launch_bounds__(1024) void embed_runs_kernel(const int32_t* __restr
     O* to = (O*)g.d_table + (size_t)v * dim + (size_t)p * N;
     float f[N];
     Piece<O, N> old;
-    if constexpr (ADD) old.template load<ODD>(to, left);
+    if constexpr (ADD) {
+      old.template load<ODD>(to, left, dim);
+      old.template settle<ODD>(left, dim);
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) f[i] = ADD ? fmaf(g.scale, sum[i], old.at(i)) : g.scale * sum[i];
     store_piece<N, ODD>(to, f, left);

@@ -42,14 +42,16 @@ template <bool ODD, int N> __device__ __forceinline__ void load_gains(const Norm
   const int left = a.dim - p * N;
   if (a.gain_bf16) {
     Piece<bf16_t, N> w;
-    w.template load<ODD>((const bf16_t*)a.gain + p * N, left);
+    w.template load<ODD>((const bf16_t*)a.gain + p * N, left, a.dim);
+    w.template settle<ODD>(left, a.dim);
 #pragma unroll
     for (int i = 0; i < N; ++i) g[i] = w.at(i);
   } else {
 #pragma unroll
     for (int k = 0; k < N; k += 4) {
       Piece<float, 4> w;
-      w.template load<ODD>((const float*)a.gain + p * N + k, left - k);
+      w.template load<ODD>((const float*)a.gain + p * N + k, left - k, a.dim);
+      w.template settle<ODD>(left - k, a.dim);
 #pragma unroll
       for (int i = 0; i < 4; ++i) g[k + i] = w.at(i);
     }
@@ -89,14 +91,16 @@ __global__ __launch_bounds__(1024) void add_norm_kernel(NormRows a, int lg) {
   for (int j = 0; j < P; ++j) {
     const int p = t + (j << lg);
     if (p < pieces) {
-      x[j].template load<ODD>((const X*)a.x + row * a.x_stride + (long long)p * N, a.dim - p * N);
-      if constexpr (ADDED) res[j].template load<ODD>((const H*)a.residual + row * a.residual_stride + (long long)p * N, a.dim - p * N);
+      x[j].template load<ODD>((const X*)a.x + row * a.x_stride + (long long)p * N, a.dim - p * N, a.dim);
+      if constexpr (ADDED) res[j].template load<ODD>((const H*)a.residual + row * a.residual_stride + (long long)p * N, a.dim - p * N, a.dim);
     }
   }
 #pragma unroll
   for (int j = 0; j < P; ++j) {
     const int p = t + (j << lg);
     if (p < pieces) {
+      x[j].template settle<ODD>(a.dim - p * N, a.dim);
+      if constexpr (ADDED) res[j].template settle<ODD>(a.dim - p * N, a.dim);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         h[j][i] = x[j].at(i);
@@ -204,15 +208,18 @@ __global__ __launch_bounds__(1024) void add_norm_grad_kernel(NormGradRows b, int
     for (int j = 0; j < P; ++j) {
       const int p = t + (j << lg);
       if (p < pieces) {
-        dy[j].template load<ODD>((const Y*)b.dy + row * b.dy_stride + (long long)p * N, a.dim - p * N);
-        h[j].template load<ODD>((const H*)b.h + row * b.h_stride + (long long)p * N, a.dim - p * N);
-        if (b.dh) dh[j].template load<ODD>((const H*)b.dh + row * b.dh_stride + (long long)p * N, a.dim - p * N);
+        dy[j].template load<ODD>((const Y*)b.dy + row * b.dy_stride + (long long)p * N, a.dim - p * N, a.dim);
+        h[j].template load<ODD>((const H*)b.h + row * b.h_stride + (long long)p * N, a.dim - p * N, a.dim);
+        if (b.dh) dh[j].template load<ODD>((const H*)b.dh + row * b.dh_stride + (long long)p * N, a.dim - p * N, a.dim);
       }
     }
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       const int p = t + (j << lg);
       if (p < pieces) {
+        dy[j].template settle<ODD>(a.dim - p * N, a.dim);
+        h[j].template settle<ODD>(a.dim - p * N, a.dim);
+        if (b.dh) dh[j].template settle<ODD>(a.dim - p * N, a.dim);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           hh = fmaf(h[j].at(i), h[j].at(i), hh);
