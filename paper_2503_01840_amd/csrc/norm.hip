@@ -263,9 +263,21 @@ __global__ __launch_bounds__(1024) void add_norm_grad_kernel(NormGradRows b, int
   }
   if (!b.partial) return;
   float* to = b.partial + (size_t)blockIdx.x * padded(a.dim);
-  if (per > 1) {                                              // rows of a workgroup one after the other
-    for (int w = 0; w < per; ++w) {
-      if (w == group) {
+  if (per > 1) {                                              // rows of a wavefront by exchanges, of a workgroup one after the other
+    if (lg < 6) {
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          if (lg <= 3) dg[j][i] += __shfl_xor(dg[j][i], 8, 64);     // step 3 is a mirror: lanes of other columns
+          if (lg <= 4) dg[j][i] = xlane_sum_step<4>(dg[j][i]);
+          dg[j][i] = xlane_sum_step<5>(dg[j][i]);
+        }
+      }
+    }
+    const int turns = lg < 6 ? blockDim.x >> 6 : per, own_turn = lg < 6 ? ((threadIdx.x & 63) >> lg ? -1 : wave) : group;
+    for (int w = 0; w < turns; ++w) {
+      if (w == own_turn) {
 #pragma unroll
         for (int j = 0; j < P; ++j) {
           const int p = t + (j << lg);
@@ -354,7 +366,9 @@ int type_size(int t) { return t == NORM_FP32 ? 4 : t == NORM_BF16 ? 2 : 1; }
 
 template <typename X, typename H, typename Y, bool ODD, int P>
 hipError_t launch_backward(const NormGradRows& b, int lg, hipStream_t st) {
-  const int threads = std::max(256, 1 << lg), per = threads >> lg;
+  // Rows that take longer by what each thread does want more threads at a time: us with 256 and 512, 65536 fp32 rows of 257 97 and 65, of 1000 on an fp32 stream 241 and 194, 16384 bf16 rows
+  // of 4095 149 and 110; but whole bf16 rows, of 1000 104 and 112, 16384 of 4096 102 and 110.
+  const int threads = std::max(piece_size<X, H, Y>() == 4 || ODD ? 512 : 256, 1 << lg), per = threads >> lg;
   // A workgroup to a CU where it has 1024 threads, else two; one also where a single round of them would leave as many parts as there are rows.  us in 512, 256, 128 parts: 512 bf16 rows
   // of 8192 20.0, 15.7, 17.9; 1024 rows 21.1, 22.1, 26.3; 8191 rows of 4096 on an fp32 stream 102, 121, 215; 2048 of 16384 138, 128
   const int blocks = (b.fwd.rows + per - 1) / per, grid = std::min(blocks, threads == 1024 || blocks <= NORM_GRAD_PARTS ? NORM_GRAD_PARTS / 2 : NORM_GRAD_PARTS);
