@@ -139,14 +139,14 @@ __device__ __forceinline__ Stat pieces_stat(const RowPieces<T>& r, int first, in
 }
 
 // ---------------------------------------------------------------- the teacher's weights of a row
-// In LDS, k of each and a table of a power of two of at least 2 k; the first wavefront of a workgroup writes and reads them, while the others' logits are on
+// In LDS, k of each and a table of a power of two, 4 k or, where k is above 512, 2048; the first wavefront of a workgroup writes and reads them, while the others' logits are on
 // their way.
 struct Teacher {
   int32_t* id;              // of the student; -1: none, or a token that occurred before
   float* p;
   float* x;                 // the student's logit of it
   float* all;               // the weights of all entries of its token
-  int32_t* first;           // by a hash of tokens: a token's first entry
+  int32_t* first;           // by a hash of tokens: the tokens, then each one's first entry
   __device__ __forceinline__ Teacher(void* lds, int k) : id((int32_t*)lds), p((float*)lds + k), x((float*)lds + 2 * k), all((float*)lds + 3 * k), first((int32_t*)lds + 4 * k) {}
 };
 __device__ __forceinline__ void wave_fence() {
@@ -204,29 +204,33 @@ __device__ __forceinline__ float weights(const DistillRows& a, long long r, cons
   for (int j = lane; j < a.k; j += 64) t.p[j] /= sum;
   return sum / sum;
 }
-// For the gradient: a token's weights to its first entry, added in the order of entries.
+// For the gradient: a token's weights to its first entry, added in the order of entries.  A chain of LDS round trips, and where rows are few what the call waits for (16 rows of 128256, 512
+// entries: 15 us; with 2 k places that hold entries, whose tokens are compared, 21).
 __device__ __forceinline__ void gather_tokens(const DistillRows& a, const Teacher& t) {
   const int lane = threadIdx.x & 63, mask = a.table - 1;
 #pragma unroll 1
-  for (int i = lane; i < a.table; i += 64) t.first[i] = -1;
+  for (int i = lane * 4; i < a.table; i += 256) *(int4*)(t.first + i) = make_int4(-1, -1, -1, -1);
   wave_fence();
-  // a place for each token: the first free one from its hash on, or that of an entry with the same token; t.all: the entry's place
+  // a place for each token: the first from its hash on that is free or the token's already; t.all: the entry's place
 #pragma unroll 1
   for (int j = lane; j < a.k; j += 64) {
     const int id = t.id[j];
-    uint32_t at = (uint32_t)id * 0x9E3779B1u >> 7;            // Fibonacci hashing
+    uint32_t at = (uint32_t)id * 0x9E3779B1u >> 7 & mask;     // Fibonacci hashing
     while (id >= 0) {
-      at &= mask;
-      const int other = atomicCAS(&t.first[at], -1, j);
-      if (other < 0) break;
-      if (t.id[other] == id) {
-        atomicMin(&t.first[at], j);
-        break;
-      }
-      ++at;
+      const int other = atomicCAS(&t.first[at], -1, id);
+      if (other < 0 || other == id) break;
+      at = (at + 1) & mask;
     }
     t.all[j] = __int_as_float((int)at);
   }
+  wave_fence();
+  // the token's first entry in its place
+#pragma unroll 1
+  for (int j = lane; j < a.k; j += 64) t.first[__float_as_int(t.all[j])] = 0x7FFFFFFF;
+  wave_fence();
+#pragma unroll 1
+  for (int j = lane; j < a.k; j += 64)
+    if (t.id[j] >= 0) atomicMin(&t.first[__float_as_int(t.all[j])], j);
   wave_fence();
 #pragma unroll 1
   for (int j0 = 0; j0 < a.k; j0 += 64) {

@@ -1003,7 +1003,7 @@ static int distill_rows(int32_t dtype, int32_t rows, int32_t vocab, const void* 
   TRY(distill_sizes(rows, vocab));
   if (!rows_fit(logits, stride, vocab, size_of(dtype))) return EAGLE3_E_SHAPE;
   a = {logits, stride, rows, vocab, t->ids, t->values, t->lse, t->t2d, t->n_t2d, t->k, t->temperature, nullptr, nullptr, nullptr, nullptr, 0, 64};
-  while (a.table < 2 * t->k) a.table *= 2;
+  while (a.table < 4 * t->k && a.table < 2048) a.table *= 2;      // an eighth to a half full
   return EAGLE3_OK;
 }
 
