@@ -441,7 +441,7 @@ typedef struct {
  * P the sum of the weights and p_v those of token v.  Rows without weights (no entry that counts, all weights zero) have loss 0 and gradient 0, rows
  * whose dloss is 0 gradient 0, whatever their logits are.
  *   logits, dtype  [rows, vocab], logits_stride elements apart;   loss  fp32 [rows]
- *   stats          fp32 [rows, 2]: a row's largest logit m and the sum of exp((x - m) / T), what the gradient needs of it; may be NULL
+ *   stats          fp32 [rows, 2], at a multiple of 8 bytes: a row's largest logit m and the sum of exp((x - m) / T), what the gradient needs of it; may be NULL
  *   dloss          DEVICE fp32 [rows]
  *   d_logits       [rows, vocab] of dtype; may be logits itself with the same stride
  * eagle3_distill_step gives loss and gradient of the same logits in one call.  eagle3_distill_grad needs no workspace.
