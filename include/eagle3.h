@@ -403,7 +403,7 @@ int eagle3_add_norm(int32_t rows, int32_t dim, int32_t x_dtype, const void* x, i
                     void* out, int64_t out_stride, eagle3_stream stream);
 
 /* The same with the norm in 8 bits, as products of 8-bit rows take it: e4m3 codes c and fp32 scales s of groups of columns, a value being s * c.  A group's
- * scale is its largest finite magnitude / 448, at least 2^-100; codes are rounded to nearest even, infinities and NaN stored as NaN.
+ * scale is its largest finite magnitude / 448, at least 2^-100; codes are the fp32 quotients of value and scale rounded to nearest even, infinities and NaN stored as NaN.
  *   group    columns to a scale: 128, or 0 for one scale a row; the last group of a row may be shorter
  *   codes    [rows, dim], codes_stride bytes apart;  scales  fp32 [rows, ceil(dim / 128)] or [rows, 1], dense */
 int eagle3_add_norm_codes(int32_t rows, int32_t dim, int32_t x_dtype, const void* x, int64_t x_stride, int32_t sum_dtype, const void* residual,

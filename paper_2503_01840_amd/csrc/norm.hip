@@ -3,7 +3,7 @@
 // A row h = x + residual is read once into the registers of its 8 to 1024 threads, its squares are summed by exchanges within the wavefronts and through LDS between
 // them, and the row is written as h and as gain * h / sqrt(mean + eps).  The gradient's rows go to at most 512 workgroups in turn, which keep the gains' gradient in
 // registers; their parts are added by a second launch (4.8 us).  Bound by bytes, at a large copy's rate and above where rows are many: 16384 rows of 8192 in bf16 178 us
-// (6.0 TB/s), 8192 of 4096 onto an fp32 stream 72 (5.6), 2048 of 8192 in 8 bits 24 (4.9), the gradient of 8191 rows of 4096 on an fp32 stream 102 (5.3).
+// (6.0 TB/s), 8192 of 4096 onto an fp32 stream 72 (5.6), 2048 of 8192 in 8 bits 25.2 (4.7), the gradient of 8191 rows of 4096 on an fp32 stream 102 (5.3).
 // Measured and not kept: an eighth of the rows to each XCD (2 to 17 % slower); the gradient's next row asked for while one is worked on (0 to 8 % slower); results stored past the
 // caches (2 to 10 % faster alone, but with an addition behind it that reads them 4096 rows of 8192 in bf16 72 -> 79 us).
 #include <algorithm>
@@ -64,10 +64,21 @@ __device__ __forceinline__ float finite_magnitude(float x) {
 }
 __device__ __forceinline__ float scale_of(float amax) { return fmaxf(amax / CODE_MOST, LEAST_SCALE); }
 
-// Two values under a scale's reciprocal as codes; what is not finite as NaN.  The product instead of a quotient moves a value by 2^-24 of it, against a
-// code's 2^-4.
-__device__ __forceinline__ uint32_t to_codes(float a, float b, float inv) {
-  const float ya = fminf(fmaxf(a * inv, -CODE_MOST), CODE_MOST), yb = fminf(fmaxf(b * inv, -CODE_MOST), CODE_MOST);
+// Values under a scale: the product with its reciprocal and one step from there, which around every border between two codes is the nearest fp32 of the quotient, so that each code is
+// the one that a division gives (the product alone, off by up to two last places, took a neighbour's now and then).  Scales below 2^-64 are raised, or what the step multiplies would leave
+// fp32's range.  2048 bf16 rows of 8192 take 25.2 us, by products alone 24.1.
+struct Quotient {
+  float raise, scale, inv;
+  __device__ __forceinline__ Quotient(float s) : raise(s < 0x1p-64f ? 0x1p64f : 1.f), scale(s * raise), inv(1.f / scale) {}
+  __device__ __forceinline__ float operator()(float x) const {
+    x *= raise;
+    const float q = x * inv;
+    return fmaf(fmaf(-q, scale, x), inv, q);
+  }
+};
+// Two values under a scale as codes; what is not finite as NaN.
+__device__ __forceinline__ uint32_t to_codes(float a, float b, const Quotient& under) {
+  const float ya = fminf(fmaxf(under(a), -CODE_MOST), CODE_MOST), yb = fminf(fmaxf(under(b), -CODE_MOST), CODE_MOST);
   uint32_t c = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(ya, yb, 0, false) & 0xFFFFu;
   if (!(fabsf(a) < __builtin_huge_valf())) c = (c & 0xFF00u) | 0x7Fu;
   if (!(fabsf(b) < __builtin_huge_valf())) c = (c & 0x00FFu) | 0x7F00u;
@@ -161,12 +172,13 @@ __global__ __launch_bounds__(1024) void add_norm_kernel(NormRows a, int lg) {
     for (int j = 0; j < P; ++j) {
       const int p = t + (j << lg);
       if (p >= pieces) continue;
-      const float scale = scale_of(a.group ? part[j] : amax), inv = 1.f / scale;
+      const float scale = scale_of(a.group ? part[j] : amax);
+      const Quotient under(scale);
       if (a.group ? p * N % 128 == 0 : p == 0) a.scales[row * n_scales + (a.group ? p * N / 128 : 0)] = scale;
       uint8_t* to = (uint8_t*)a.out + row * a.out_stride + (long long)p * N;
       typename Words<N>::type c;
-      if constexpr (N == 8) c = u32x2_t{to_codes(h[j][0], h[j][1], inv) | to_codes(h[j][2], h[j][3], inv) << 16, to_codes(h[j][4], h[j][5], inv) | to_codes(h[j][6], h[j][7], inv) << 16};
-      else c = to_codes(h[j][0], h[j][1], inv) | to_codes(h[j][2], h[j][3], inv) << 16;
+      if constexpr (N == 8) c = u32x2_t{to_codes(h[j][0], h[j][1], under) | to_codes(h[j][2], h[j][3], under) << 16, to_codes(h[j][4], h[j][5], under) | to_codes(h[j][6], h[j][7], under) << 16};
+      else c = to_codes(h[j][0], h[j][1], under) | to_codes(h[j][2], h[j][3], under) << 16;
       if constexpr (!ODD) {
         *(typename Words<N>::type*)to = c;
       } else if (a.dim - p * N >= N) {

@@ -99,6 +99,26 @@ def test_norm_in_8_bits(rows, dim, types, group):
         assert bool(((c - q).abs() <= step / 2 + q.abs() * (2 * NORM + 4 * U)).all()) and bool((c.abs() <= 448).all())
 
 
+@pytest.mark.parametrize("dim", [1000, 4096, 129])
+@every(group=[0, 128], xt=[BF16, FP32], exponent=[0, -60, -90, 60])
+def test_codes_are_those_of_a_division(dim, group, xt, exponent):
+    """Values one last place around the borders between two codes.  Rows of 1 and -1 have a mean square and a root of 1, whatever order they are summed in, so a norm is its gain, and code and scale are
+    known to the last bit: that of the fp32 quotient, to nearest even."""
+    g = torch.Generator().manual_seed(dim)
+    x = (torch.randint(0, 2, (40, dim), generator=g) * 2 - 1).to(xt)
+    width = group or dim
+    most = torch.cat([((1 + torch.rand(1, generator=g)) * 2.0 ** exponent).expand(min(width, dim - at)) for at in range(0, dim, width)])
+    scale = most / 448
+    borders = torch.cat([torch.tensor([2.0 ** e * (17 + 2 * m) / 16 for e in range(-6, 8) for m in range(8)]), torch.arange(1, 16, 2) * 2.0 ** -10])
+    gain = borders[torch.randint(0, len(borders), (dim,), generator=g)] * scale
+    away = torch.randint(-1, 2, (dim,), generator=g)
+    gain = torch.where(away > 0, torch.nextafter(gain, torch.tensor(math.inf)), torch.where(away < 0, torch.nextafter(gain, torch.tensor(0.0)), gain)).minimum(most)
+    gain[::width] = most[::width]
+    codes, scales = E.eagle3_add_norm_codes(x.to(DEV), gain.to(DEV), 0.0, group=group)
+    assert torch.equal(scales.cpu(), scale[::width].expand(40, -1))
+    assert torch.equal(codes.cpu().float(), x.float() * (gain / scale).to(torch.float8_e4m3fn).float())
+
+
 def test_codes_of_rows_that_hold_no_numbers_or_nothing():
     """Zeros, tiny values, one huge one, infinities and NaN."""
     for dim in (256, 250):
