@@ -285,10 +285,10 @@ __global__ __launch_bounds__(THREADS) void distill_part_kernel(DistillRows a, fl
   if (threadIdx.x == 0) *(float2*)(partial + ((size_t)r * gridDim.z + blockIdx.z) * 2) = make_float2(st.m, st.s);
 }
 
-// Loss and stats of a row, from the row itself or (parts > 0) from those of its parts.  dynamic LDS here and below: the teacher's
+// Loss and stats of a row, from the row itself or (parts > 0) from those of its parts.  dynamic LDS here and below: the teacher's, at a multiple of 16 bytes, by which it is cleared
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void distill_loss_kernel(DistillRows a, float c, const float* partial, int parts) {
-  extern __shared__ uint32_t lds[];
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   __shared__ float red[2][16];
   const Teacher t(lds, a.k);
   const long long r = (long long)blockIdx.y * gridDim.x + blockIdx.x;
@@ -339,7 +339,7 @@ template <typename T> __device__ __forceinline__ void write_single(const RowPiec
 // teacher's weights are formed.
 template <typename T, int THREADS, int R, bool EVEN>
 __global__ __launch_bounds__(THREADS) void distill_grad_kernel(DistillRows a, float c, int share) {
-  extern __shared__ uint32_t lds[];
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   __shared__ float sum_of_weights;
   const Teacher t(lds, a.k);
   const long long r = (long long)blockIdx.y * gridDim.x + blockIdx.x;
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(THREADS) void distill_grad_kernel(DistillRows a, fl
 // them is read twice.
 template <typename T, int THREADS, int R, int Q, int WAVES, bool EVEN>
 __global__ __launch_bounds__(THREADS, WAVES) void distill_step_kernel(DistillRows a, float c) {
-  extern __shared__ uint32_t lds[];
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   __shared__ float red[2][16], sum_of_weights;
   const Teacher t(lds, a.k);
   const long long r = (long long)blockIdx.y * gridDim.x + blockIdx.x;
