@@ -120,6 +120,14 @@ def test_loss_and_gradient(case, dtype):
     assert bool((grad[none.to(DEV)] == 0).all()) and bool((got[none.to(DEV)] == 0).all())
 
 
+@pytest.mark.parametrize("rows,V,k,dtype,tail,mapped", [(64, 70001, 40, FP32, False, False), (66, 98304, 1024, FP32, True, True), (65, 128256, 1024, FP32, True, False), (67, 131071, 128, BF16, True, False),
+                                                        (64, 140001, 300, BF16, False, True), (65, 210003, 1024, BF16, True, False)])
+def test_long_rows_in_one_launch(rows, V, k, dtype, tail, mapped):
+    """Rows that are not worked on in parts and have more pieces than a workgroup's registers hold (16384): up to 24576 of them stay in LDS behind the teacher's tables, of which the largest are among
+    these, and what is behind is read twice; and rows of 16 bits just below the first line."""
+    test_loss_and_gradient((rows, V, k, tail, mapped, 1.0), dtype)
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("rows,V", [(3, 1001), (5, 40003), (1025, 1003), (1024, 33001)])
 def test_rows_that_lie_apart(rows, V, dtype):
