@@ -158,6 +158,25 @@ def test_rows_that_lie_apart(rows, V, dtype):
         assert torch.equal(view, out if off == out_off else view) and bool((wide[:, :off] == 30).all()) and bool((wide[:, off + V:] == 30).all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows,V", [(3, 1001), (5, 40003), (1025, 1003), (64, 70003)])
+def test_gradients_over_logits_that_start_anywhere(rows, V, dtype):
+    """Over the logits, at any distance from a multiple of 16 bytes, against the definition: in one call, and from the stats."""
+    g = torch.Generator().manual_seed(V + 1)
+    x, ids, values, lse, _ = _case(g, rows, V, 9, dtype, True, False, 1.0)
+    dloss = torch.randn(rows, generator=g).to(DEV)
+    ref = _reference(x, ids, values, lse, None, 1.0, dloss)
+    _, stats = E.eagle3_distill(x, ids, values, lse, want_stats=True)
+    for off, width in ((0, V + 7), (1, V + 13), (3, V + 16), (5, V + 9), (7, V + 8)):
+        for call in (lambda o: E.eagle3_distill_step(dloss, o, ids, values, lse, out=o)[1], lambda o: E.eagle3_distill_grad(dloss, stats, o, ids, values, lse, out=o)):
+            wide = torch.full((rows, width), 30.0, dtype=dtype, device=DEV)
+            view = wide[:, off:off + V]
+            view.copy_(x)
+            assert call(view) is view
+            _check(view, ref[1], ref[3], dtype)
+            assert bool((wide[:, :off] == 30).all()) and bool((wide[:, off + V:] == 30).all())
+
+
 @pytest.mark.parametrize("rows,V", [(8, 300), (8, 50000), (1032, 9000)])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_masked_infinite_and_missing_values(rows, V, dtype):
