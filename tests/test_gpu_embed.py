@@ -102,6 +102,12 @@ def test_gradient_of_the_table(rows, dim, vocab, types, how):
     _check_grad(both, dy, tok, vocab, -0.7, old)
 
 
+@pytest.mark.parametrize("rows,dim,vocab", [(12288, 24, 511), (12289, 40, 511), (16385, 16, 512), (12289, 72, 513), (13000, 24, 300), (13000, 12, 1), (20480, 8, 262143), (20481, 8, 262144)])
+def test_gradients_of_rows_sorted_by_digits(rows, dim, vocab):
+    """More rows than are ranked (12288): vocabularies of one, two and three digits on both sides of the lines between these, whole and broken tiles of 4096."""
+    test_gradient_of_the_table(rows=rows, dim=dim, vocab=vocab)
+
+
 @pytest.mark.parametrize("dim", [64, 61])
 @pytest.mark.parametrize("how", ["apart", "off"])
 def test_gradients_of_rows_that_lie_apart(dim, how):
