@@ -200,3 +200,34 @@ def test_captured_gradients_replay():
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, want)), i
             (torch.randn(1000, device=DEV) * 2).sum()
+
+
+@pytest.mark.parametrize("rows", [1, 300, 384, 385, 12288, 12289, 13000, 20000])
+def test_every_way_of_sorting_replays(rows):
+    """Token by token in one launch, by ranks and by one and two digits: other tokens and gradients at every replay, against eager calls."""
+    g = torch.Generator().manual_seed(rows)
+    tok = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    dy, old = torch.zeros(rows, 40, device=DEV), torch.randn(1500, 40, generator=g).to(DEV)
+
+    def step():
+        return [E.eagle3_embed_grad(dy, tok, v) for v in (300, 1500)] + [E.eagle3_embed_grad(dy, tok, 1500, out=old.clone(), accumulate=True)]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for i in range(4):
+        tok.copy_(torch.randint(-3, 1510 // (i + 1), (rows,), generator=g, dtype=torch.int32))
+        dy.copy_(torch.randn(rows, 40, generator=g))
+        old.copy_(torch.randn(1500, 40, generator=g))
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+        (torch.randn(1000, device=DEV) * 2).sum()
+    _check_grad(got[1], dy, tok, 1500, 1.0)
+    _check_grad(got[2], dy, tok, 1500, 1.0, old)
