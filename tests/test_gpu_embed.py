@@ -65,6 +65,21 @@ def test_rows_of_the_table(rows, dim, vocab, types, how):
     assert new.is_contiguous() and new.dtype == types[1] and torch.equal(new, got)
 
 
+@pytest.mark.parametrize("rows,dim,types", [(8192, 8192, (BF16, BF16)), (8193, 8192, (BF16, BF16)), (4096, 8192, (FP32, FP32)), (4099, 8200, (BF16, FP32)), (16384, 4096, (FP32, BF16))])
+def test_large_results(rows, dim, types):
+    """Results of 128 MiB and more, which are stored past the caches, and what reads them next."""
+    g = torch.Generator().manual_seed(rows)
+    table = torch.randn(1000, dim, generator=g).to(types[0]).to(DEV)
+    tok = _tokens(g, rows, 1000, "ends").to(DEV)
+    got = E.eagle3_embed(table, tok, 0.37, dtype=types[1])
+    back = got + 0
+    assert got.numel() * got.element_size() >= 128 << 20 and torch.equal(got, back)
+    seen = (tok >= 0) & (tok < 1000)
+    for at in range(0, rows, 1024):
+        want = torch.where(seen[at:at + 1024, None], table[tok[at:at + 1024].long().clamp(0, 999)].double() * torch.tensor(0.37, dtype=FP32).double(), 0.0)
+        assert bool(((got[at:at + 1024].double() - want).abs() <= want.abs() * U + _out(types[1], want * (1 + U))).all())
+
+
 def _check_grad(got, dy, tok, vocab, scale, old=None):
     """Sums of a token's n rows in any order: (n - 1) roundings of partial sums, the factor, an addition to what was there; one rounding to the type."""
     dy, tok = dy.double().cpu(), tok.long().cpu()
