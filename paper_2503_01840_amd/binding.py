@@ -9,6 +9,7 @@ import ctypes as C
 import os
 
 import torch
+from torch.autograd import forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libeagle3.so")
@@ -417,6 +418,14 @@ def _refuse(what, wanted, t):
     raise ValueError(f"{what}: {wanted} is wanted, got " + (f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}" if isinstance(t, torch.Tensor) else repr(t)))
 
 
+def _no_tangents(what, *tensors):
+    """The calls that are recorded for autograd have gradients, but no forward-mode derivatives: without this, a dual tensor's tangent would be lost without a word."""
+    if forward_ad._current_level >= 0:                        # a dual_level() is open, which is hardly ever so
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                _refuse(what, "a tensor without a forward-mode tangent", t)
+
+
 def _arg(t, dtype, shape, gpu, what):
     """The address of a dense tensor of this type and shape on GPU number `gpu`."""
     if t.dtype is not dtype or t.get_device() != gpu or t.shape != shape or not t.is_contiguous():
@@ -528,6 +537,7 @@ class _Turned(torch.autograd.Function):
 
 
 def _turn(call, back, rope, positions, q, k, out):
+    _no_tangents("q, k, out", q, k, *(out if isinstance(out, (tuple, list)) else (out,)))
     wanted = q.requires_grad or (k is not None and k.requires_grad)
     if out is not None:
         wanted = wanted or any(t is not None and t.requires_grad for t in (out if isinstance(out, (tuple, list)) else (out,)))
@@ -713,6 +723,7 @@ def _workspace(call, sizes, like):
 
 
 def _recorded(*tensors):
+    _no_tangents("inputs", *tensors)
     for t in tensors:
         if t is not None and t.requires_grad:
             return torch.is_grad_enabled()
@@ -765,7 +776,7 @@ def eagle3_embed(table, tokens, scale=1.0, dtype=None, out=None):
         _type(dtype, "dtype")
     if out is not None:
         _not_over_records(out, table)
-    elif table.requires_grad and torch.is_grad_enabled():
+    elif _recorded(table):
         return _Embedded.apply(table, tokens, scale, dtype)
     return _embed(table, tokens, scale, dtype, out)
 
@@ -906,6 +917,7 @@ def _teacher(logits, ids, values, lse, t2d, temperature):
     """(gpu, sizes and logits as the calls take them, the teacher's struct)"""
     gpu = _gpu_of(logits, "logits")
     xp, n, V, xs, xc = _table(logits, gpu, "logits")
+    _no_tangents("values, lse", values, lse)
     if ids.dim() != 2 or values.requires_grad or (lse is not None and lse.requires_grad):
         _refuse("ids, values, lse", "int32 [rows, k], and fp32 values of which no gradient is wanted", ids)
     k = ids.shape[1]
@@ -943,7 +955,7 @@ def eagle3_distill(logits, ids, values, lse=None, t2d=None, temperature=1.0, wan
     """The cross entropy, fp32 [rows], of a student's logits [rows, vocab] (bf16 or fp32, rows any distance apart) against a teacher's logits `values` fp32 [rows, k] of
     the tokens `ids` int32 [rows, k] (include/eagle3.h: eagle3_teacher): the teacher's probabilities among these tokens, or with lse fp32 [rows] those that it gave
     them; t2d int32 [n]: the student's ids of the teacher's tokens.  With want_stats (loss, stats fp32 [rows, 2]).  Recorded for autograd."""
-    if logits.requires_grad and torch.is_grad_enabled():
+    if _recorded(logits):
         got = _Distilled.apply(logits, ids, values, lse, t2d, temperature)
         return got if want_stats else got[0]
     got = _distill(logits, ids, values, lse, t2d, temperature, want_stats)

@@ -200,3 +200,40 @@ def test_what_is_written_over_is_known_to_a_backward_pass(sent):
         before = x._version
         call()
         assert x._version == before + 1
+
+
+def _recorded_calls(mark):
+    """Each input of the calls that are recorded, and what is written through `out`, as `mark` gives it."""
+    z = lambda *shape: torch.zeros(*shape)
+    x, gain, table, tok, ids, values = z(4, 16), z(16), z(9, 16), torch.zeros(4, dtype=torch.int32), torch.zeros(4, 2, dtype=torch.int32), z(4, 2)
+    return [lambda: E.eagle3_embed(mark(table), tok), lambda: E.eagle3_embed(mark(table), tok, 2.0, torch.bfloat16), lambda: E.eagle3_embed(mark(table), tok, out=z(4, 16)),
+            lambda: E.eagle3_embed(table, tok, out=mark(x)), lambda: E.eagle3_add_norm(mark(x), gain, 1e-5), lambda: E.eagle3_add_norm(x, mark(gain), 1e-5),
+            lambda: E.eagle3_add_norm(x, gain, 1e-5, residual=mark(z(4, 16))), lambda: E.eagle3_add_norm(mark(x), gain, 1e-5, out=z(4, 16)), lambda: E.eagle3_distill(mark(x), ids, values),
+            lambda: E.eagle3_distill(x, ids, mark(values)), lambda: E.eagle3_distill(x, ids, values, lse=mark(z(4))), lambda: E.eagle3_distill(mark(x), ids, values, want_stats=True)]
+
+
+def test_forward_mode_derivatives_are_refused(sent):
+    """A dual tensor would come back without its tangent: derivatives of 0, with no error."""
+    from torch.autograd import forward_ad
+    dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))
+    for call in _recorded_calls(dual):
+        for mode in (torch.enable_grad, torch.no_grad):       # tangents are carried on in either
+            with forward_ad.dual_level(), mode(), pytest.raises(ValueError, match="forward-mode"):
+                call()
+    for call in (lambda t: E.eagle3_embed(t, torch.zeros(4, dtype=torch.int32)), lambda t: E.eagle3_add_norm(t, torch.ones(16), 1e-5),
+                 lambda t: E.eagle3_distill(t, torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2))):
+        with pytest.raises(Exception):
+            torch.func.jvp(call, (torch.zeros(4, 16),), (torch.ones(4, 16),))
+    q = torch.zeros(4, 2, 16)
+    for call in (E.eagle3_rope, E.eagle3_rope_grad):
+        for args in (lambda: (dual(q),), lambda: (q, dual(q)), lambda: (q, None, dual(q)), lambda: (q, q, (q.clone(), dual(q)))):
+            with forward_ad.dual_level(), pytest.raises(ValueError, match="forward-mode"):
+                call(None, torch.zeros(4, dtype=torch.int32), *args())
+    assert not sent
+    # an open level does no harm to other tensors, and a dual tensor none behind it
+    with forward_ad.dual_level():
+        kept = dual(torch.zeros(4, 16))
+        for call in _recorded_calls(lambda t: t):
+            call()
+    E.eagle3_add_norm(kept, torch.ones(16), 1e-5)
+    assert len(sent) == 13
