@@ -374,7 +374,7 @@ int eagle3_paged_attention_workspace(const eagle3_paged_kv* kv, int32_t B, int32
  * taught by the target's), and for layers of a program's own.  No call needs a context.  Types are EAGLE3_BF16 and EAGLE3_FP32 throughout; sums are
  * formed in 32 bits, results rounded once.  No result depends on the order in which workgroups run.  Rows lie `stride` elements apart (at least their
  * length, below 2^40) and may start at any multiple of their type's size; rows at multiples of 16 bytes are the fast ones.  Outputs do not overlap
- * inputs except where that is said.  A workspace is DEVICE memory, 256-byte aligned, of the bytes that the call's _workspace tells for the same sizes;
+ * inputs or each other except where that is said.  A workspace is DEVICE memory, 256-byte aligned, of the bytes that the call's _workspace tells for the same sizes;
  * its content need not be kept or cleared between calls, and calls that may overlap in time need one each. */
 
 /* Rows of an embedding table, times a factor: out[r] = scale * table[tokens[r]].  Tokens outside 0..vocab-1 are padding: rows of zeros.
@@ -415,7 +415,7 @@ int eagle3_add_norm_codes(int32_t rows, int32_t dim, int32_t x_dtype, const void
  * d_sum is the gradient of x and of residual alike.
  *   h, dh, d_sum   [rows, dim] of sum_dtype; dh may be NULL (no further use) or d_sum itself with the same stride; d_sum may be NULL if dx is not
  *   dy, dy_dtype   [rows, dim], as out was
- *   dx, x_dtype    [rows, dim] or NULL: d_sum once more, in the type of x
+ *   dx, x_dtype    [rows, dim] or NULL: d_sum once more, in the type of x; may be d_sum itself with the same type and stride
  *   d_gain         [dim] of gain_dtype, or NULL
  * Sizes as above. */
 int eagle3_add_norm_grad(int32_t rows, int32_t dim, int32_t dy_dtype, const void* dy, int64_t dy_stride, int32_t sum_dtype, const void* h,

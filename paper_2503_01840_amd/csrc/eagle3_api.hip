@@ -894,6 +894,16 @@ static int64_t size_of(int32_t t) { return t == EAGLE3_FP32 ? 4 : 2; }
 // Rows of n elements of `size` bytes that the kernels can address.
 static bool rows_fit(const void* p, int64_t stride, int64_t n, int64_t size) { return stride >= n && stride < (int64_t)1 << 40 && (uintptr_t)p % size == 0; }
 
+// Whether two results of `rows` rows of p_bytes and q_bytes are written over each other: rows equally far apart that share a byte, others that begin at one place.
+static bool rows_meet(const void* p, int64_t p_stride, int64_t p_bytes, const void* q, int64_t q_stride, int64_t q_bytes, int64_t rows) {
+  const int64_t apart = (int64_t)((uintptr_t)q - (uintptr_t)p);
+  if (rows == 1) return apart < p_bytes && -apart < q_bytes;
+  if (p_stride != q_stride) return apart == 0;
+  // row r of q begins `at` bytes behind the beginning of row r + down of p, and p_stride - at in front of that of the next one
+  const int64_t down = apart >= 0 ? apart / p_stride : -((p_stride - 1 - apart) / p_stride), at = apart - down * p_stride;
+  return (at < p_bytes && down < rows && -down < rows) || (p_stride - at < q_bytes && down + 1 < rows && -down - 1 < rows);
+}
+
 static int workspace_fits(const void* workspace, size_t bytes, size_t need) {
   return need > bytes || (need && (!workspace || ((uintptr_t)workspace & 255))) ? EAGLE3_E_STATE : EAGLE3_OK;
 }
@@ -954,6 +964,8 @@ int eagle3_add_norm(int32_t rows, int32_t dim, int32_t x_dtype, const void* x, i
   TRY(norm_rows(a, x_dtype, sum_dtype, gain_dtype));
   if (!real_type(out_dtype) || !rows_fit(out, out_stride, dim, size_of(out_dtype))) return EAGLE3_E_SHAPE;
   if (out == x && (out_dtype != x_dtype || out_stride != x_stride)) return EAGLE3_E_SHAPE;
+  const int64_t h = size_of(sum_dtype), y = size_of(out_dtype);
+  if (residual && rows_meet(sum_out, sum_stride * h, dim * h, out, out_stride * y, dim * y, rows)) return EAGLE3_E_SHAPE;
   CK(launch_norm_rows(a, norm_type(x_dtype), norm_type(residual ? sum_dtype : x_dtype), norm_type(out_dtype), (hipStream_t)stream));
   return EAGLE3_OK;
 }
@@ -965,6 +977,7 @@ int eagle3_add_norm_codes(int32_t rows, int32_t dim, int32_t x_dtype, const void
   if (!scales) return EAGLE3_E_NULL;
   TRY(norm_rows(a, x_dtype, sum_dtype, gain_dtype));
   if ((group != 0 && group != 128) || !rows_fit(codes, codes_stride, dim, 1) || (uintptr_t)scales % 4) return EAGLE3_E_SHAPE;
+  if (residual && rows_meet(sum_out, sum_stride * size_of(sum_dtype), dim * size_of(sum_dtype), codes, codes_stride, dim, rows)) return EAGLE3_E_SHAPE;
   CK(launch_norm_rows(a, norm_type(x_dtype), norm_type(residual ? sum_dtype : x_dtype), NORM_CODES, (hipStream_t)stream));
   return EAGLE3_OK;
 }
@@ -988,6 +1001,9 @@ int eagle3_add_norm_grad(int32_t rows, int32_t dim, int32_t dy_dtype, const void
   if (!(eps >= 0.f) || !rows_fit(gain, dim, dim, size_of(gain_dtype)) || !rows_fit(dy, dy_stride, dim, size_of(dy_dtype)) || !rows_fit(h, h_stride, dim, s)) return EAGLE3_E_SHAPE;
   if ((dh && !rows_fit(dh, dh_stride, dim, s)) || (d_sum && !rows_fit(d_sum, d_sum_stride, dim, s)) || (dx && !rows_fit(dx, dx_stride, dim, size_of(x_dtype)))) return EAGLE3_E_SHAPE;
   if ((dh && d_sum == dh && d_sum_stride != dh_stride) || (uintptr_t)d_gain % size_of(gain_dtype)) return EAGLE3_E_SHAPE;
+  const int64_t x = size_of(x_dtype);
+  const bool twice = d_sum == dx && x_dtype == sum_dtype && d_sum_stride == dx_stride;         // the same rows, of the same type
+  if (d_sum && dx && !twice && rows_meet(d_sum, d_sum_stride * s, dim * s, dx, dx_stride * x, dim * x, rows)) return EAGLE3_E_SHAPE;
   if (d_gain) TRY(workspace_fits(workspace, workspace_bytes, norm_grad_workspace(rows, dim)));
   const NormRows a = {nullptr, nullptr, nullptr, gain, nullptr, nullptr, 0, 0, 0, 0, rows, dim, 0, gain_dtype == EAGLE3_BF16, eps};
   CK(launch_norm_rows_grad({a, dy, h, dh, d_sum, dx, d_gain, d_gain ? (float*)workspace : nullptr, dy_stride, h_stride, dh_stride, d_sum_stride, dx_stride},

@@ -83,6 +83,31 @@ def test_gradients_of_norms(L, over, code):
     assert L.eagle3_add_norm_grad(*_args(NORM_GRAD, over)) == code
 
 
+def test_results_over_each_other(L):
+    """Norm and sum, codes and sum, and the two gradients, in rows of one buffer: refused where a byte is written by both."""
+    apart = dict(h=AT + 65536, out=AT + 131072)
+    for over in (dict(out=AT + 65536), dict(out=AT + 65536, out_dtype=0), dict(out=AT + 65536 + 64, out_dtype=0), dict(out=AT + 65536 - 4, out_dtype=0), dict(out=AT + 65536 + 192, out_dtype=0),
+                 dict(out=AT + 65536 + 256, out_dtype=0), dict(out=AT + 65536, os=70), dict(rows=1, out=AT + 65536 + 252, hs=99), dict(rows=1, out=AT + 65536 - 126, os=99)):
+        assert L.eagle3_add_norm(*_args(NORM, {**apart, **over})) == -2, over
+    for over in (dict(codes=AT + 65536), dict(codes=AT + 65536, cs=256), dict(codes=AT + 65536 + 255, cs=256), dict(codes=AT + 65536 - 63, cs=256), dict(rows=1, codes=AT + 65536 + 255)):
+        assert L.eagle3_add_norm_codes(*_args(CODES, {"h": AT + 65536, **over})) == -2, over
+    # every place of dx around d_sum against the bytes themselves; without a workspace nothing is enqueued in any case
+    size = {0: 4, 1: 2}
+    for rows, stride in ((1, 5), (2, 3), (2, 7), (3, 5)):
+        for sum_t, x_t in ((0, 0), (1, 1), (0, 1)):
+            for x_stride in {stride, stride * size[sum_t] // size[x_t]}:
+                if x_stride < 3:
+                    continue
+                bytes_of = lambda at, s, t: {at + r * s * size[t] + b for r in range(rows) for b in range(3 * size[t])}
+                for off in range(-40, 42, 2 if x_t else 4):
+                    both = dict(rows=rows, dim=3, dys=3, hs=3, dh=None, sum_dtype=sum_t, d_sum=AT + 65536, dss=stride, x_dtype=x_t, dx=AT + 65536 + off, dxs=x_stride, ws=None)
+                    meet = bool(bytes_of(0, stride, sum_t) & bytes_of(off, x_stride, x_t))
+                    if rows > 1 and stride * size[sum_t] != x_stride * size[x_t]:
+                        meet = off == 0                       # rows not equally far apart: known by their beginning only
+                    same = off == 0 and sum_t == x_t and stride == x_stride
+                    assert L.eagle3_add_norm_grad(*_args(NORM_GRAD, both)) == (-2 if meet and not same else -3), both
+
+
 def _teacher(**over):
     v = dict(ids=AT, values=AT, lse=None, t2d=None, n_t2d=0, k=4, temperature=1.0)
     v.update(over)

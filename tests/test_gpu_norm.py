@@ -230,6 +230,21 @@ def test_autograd_and_differences():
         y.sum().backward()
 
 
+@pytest.mark.parametrize("dim", [64, 61])
+def test_norm_and_sum_side_by_side(dim):
+    """Both results in rows of one buffer, and refused where they share columns of it."""
+    g = torch.Generator().manual_seed(dim)
+    x, res, gain = torch.randn(40, dim, generator=g).to(DEV), torch.randn(40, dim, generator=g).to(DEV), torch.randn(dim, generator=g).to(DEV)
+    want = E.eagle3_add_norm(x, gain, EPS, residual=res)
+    t = torch.full((40, 2 * dim), 5.0, device=DEV)
+    got = E.eagle3_add_norm(x, gain, EPS, residual=res, out=(t[:, dim:], t[:, :dim]))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(t, torch.cat([want[1], want[0]], 1))
+    for over in ((t[:, :dim], t[:, :dim]), (t[:, 1:dim + 1], t[:, :dim]), (t[1:, dim - 1:-1], t[:-1, :dim])):
+        with pytest.raises(E.Eagle3Error):
+            E.eagle3_add_norm(x[:len(over[0])], gain, EPS, residual=res[:len(over[0])], out=over)
+    assert torch.equal(t, torch.cat([want[1], want[0]], 1))
+
+
 def test_infinities_stay_in_their_row():
     x = torch.randn(6, 300, generator=torch.Generator().manual_seed(2)).to(DEV)
     x[1, 4], x[3, 299] = float("inf"), float("nan")
