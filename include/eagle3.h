@@ -413,7 +413,8 @@ int eagle3_add_norm_codes(int32_t rows, int32_t dim, int32_t x_dtype, const void
 /* The gradient of eagle3_add_norm, from that of out (dy) and, where the sum is used further on, that of the sum (dh):
  *   d_sum = dh + r (gain dy - h r^2 mean(gain dy h)),  r = 1 / sqrt(mean(h^2) + eps);   d_gain = sum over rows of dy h r
  * d_sum is the gradient of x and of residual alike.
- *   h, dh, d_sum   [rows, dim] of sum_dtype; dh may be NULL (no further use) or d_sum itself with the same stride; d_sum may be NULL if dx is not
+ *   h, dh, d_sum   [rows, dim] of sum_dtype, h as sum_out has it: the gradient is that of the row as it was rounded to the stream's type, which in bf16 is not to the
+ *                  last bit the one that was normalised; dh may be NULL (no further use) or d_sum itself with the same stride; d_sum may be NULL if dx is not
  *   dy, dy_dtype   [rows, dim], as out was
  *   dx, x_dtype    [rows, dim] or NULL: d_sum once more, in the type of x; may be d_sum itself with the same type and stride
  *   d_gain         [dim] of gain_dtype, or NULL

@@ -866,7 +866,8 @@ class _Normed(torch.autograd.Function):
 def eagle3_add_norm(x, gain, eps, residual=None, dtype=None, out=None):
     """gain * h / sqrt(mean(h^2) + eps) of the rows h = x + residual, [rows, dim] of `dtype` (None: that of x).  x [rows, dim], residual the same in x's type
     or fp32, gain [dim]; bf16 or fp32, rows any distance apart.  Returns the norm, with residual (norm, h in residual's type).  `out`: the norm's
-    tensor, or (the norm's or None, the sum's or None), which may be x and residual themselves.  Recorded for autograd, which `out` does not allow."""
+    tensor, or (the norm's or None, the sum's or None), which may be x and residual themselves.  Recorded for autograd, which `out` does not allow;
+    the backward pass takes h as it was rounded to its type."""
     if dtype is not None:
         _type(dtype, "dtype")
     if out is not None:

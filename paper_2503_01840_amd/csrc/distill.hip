@@ -139,7 +139,7 @@ __device__ __forceinline__ Stat pieces_stat(const RowPieces<T>& r, int first, in
 }
 
 // ---------------------------------------------------------------- the teacher's weights of a row
-// In LDS, k of each and a table of a power of two, 4 k or, where k is above 512, 2048; the first wavefront of a workgroup writes and reads them, while the others' logits are on
+// In LDS, k of each and a table: the power of two from 4 k on, at least 64 and at most 2048 places; the first wavefront of a workgroup writes and reads them, while the others' logits are on
 // their way.
 struct Teacher {
   int32_t* id;              // of the student; -1: none, or a token that occurred before

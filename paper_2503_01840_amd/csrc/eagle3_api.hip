@@ -1019,7 +1019,7 @@ static int distill_rows(int32_t dtype, int32_t rows, int32_t vocab, const void* 
   TRY(distill_sizes(rows, vocab));
   if (!rows_fit(logits, stride, vocab, size_of(dtype))) return EAGLE3_E_SHAPE;
   a = {logits, stride, rows, vocab, t->ids, t->values, t->lse, t->t2d, t->n_t2d, t->k, t->temperature, nullptr, nullptr, nullptr, nullptr, 0, 64};
-  while (a.table < 4 * t->k && a.table < 2048) a.table *= 2;      // an eighth to a half full
+  while (a.table < 4 * t->k && a.table < 2048) a.table *= 2;      // at most a quarter full, beyond 512 entries a half
   return EAGLE3_OK;
 }
 

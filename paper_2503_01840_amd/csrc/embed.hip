@@ -7,7 +7,8 @@
 // digits of at most 9 bits in two launches each.  Workgroups behind those that sort write zeros to the table meanwhile.  Then CHUNK sorted places at a time are summed by a wavefront for 64
 // pieces of columns, all CHUNK rows on their way at once; a token's sum that lies within them is written at once, the ends of one that does not go to the workspace and are added by the
 // last launch; few rows are summed in one launch, token by token.  Bound by bytes, of which a large table's zeros are nearly all: 8192 rows of 4096 into 128256 in bf16 158 us for tokens and zeros (1051 MB, 6.7 TB/s), 17 and 6 for the sums;
-// 1021 fp32 rows of 251 into 2048 6.2, 7.6 and 3.1, three launches that wait for memory.
+// 1021 fp32 rows of 251 into 2048 6.3, 7.9 and 3.6, three launches that wait for memory.  Added to a table that is there: 8192 rows of 4096 47 us, where the sort has no zeros above it, 16384 rows 79,
+// of 256 columns 35, of which sorting by two digits is 23 (counts 3.0 each, places 8.6).
 // Measured and not kept: one launch without sorted tokens for up to 1024 rows, each workgroup looking through all tokens for its part of the table (1021 rows of 251: 16.8 -> 15.4 us, but
 // 33 where half of the rows have one token, 61 where all have; tables of 1 GB 168 -> 171); zeros by the launch that sums; a token's rows 8 or 32 at a time.
 #include <algorithm>
@@ -371,6 +372,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restri
 // Few rows: no parts and no second launch.  A workgroup has the tokens whose first place is one of CHUNK, a wavefront each; one with more than 64 rows, the last, is summed by all wavefronts, a
 // 16th of its places each.  With one token in many rows a CU draws them alone, so this is for few: us, sums and parts in two launches against this, tokens of a log-uniform rank and one token
 // in all rows: 300 rows of 4096 20.4 and 16.3, 19.9 and 19.3; 400 20.5 and 17.2, 20.4 and 21.0; 512 20.6 and 17.2, 21.2 and 26.8; 2048 25.5 and 28.2, 32.1 and 66.9.
+// 16 registers of a thread are spilled where odd bf16 rows are added to a bf16 table.
 constexpr int RUN_ROWS = 384;
 template <typename T, typename O, bool ODD, bool ADD>
 __global__ __launch_bounds__(1024) void embed_runs_kernel(const int32_t* __restrict__ token, const int32_t* __restrict__ row_of, int n, int dim, int vocab, EmbedGrad g) {

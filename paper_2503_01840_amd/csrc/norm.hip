@@ -2,10 +2,12 @@
 //
 // A row h = x + residual is read once into the registers of its 8 to 1024 threads, its squares are summed by exchanges within the wavefronts and through LDS between
 // them, and the row is written as h and as gain * h / sqrt(mean + eps).  The gradient's rows go to at most 512 workgroups in turn, which keep the gains' gradient in
-// registers; their parts are added by a second launch (4.8 us).  Bound by bytes, at a large copy's rate and above where rows are many: 16384 rows of 8192 in bf16 178 us
-// (6.0 TB/s), 8192 of 4096 onto an fp32 stream 72 (5.6), 2048 of 8192 in 8 bits 25.2 (4.7), the gradient of 8191 rows of 4096 on an fp32 stream 102 (5.3).
+// registers; their parts are added by a second launch (4.8 us).  Bound by bytes, at a large copy's rate and above where rows are many: 16384 rows of 8192 in bf16 180 to 182 us
+// (5.9 TB/s), 8192 of 4096 onto an fp32 stream 72 (5.6), 2048 of 8192 in 8 bits 25.2 (4.7), the gradient of 8191 rows of 4096 on an fp32 stream 102 (5.3).
 // Measured and not kept: an eighth of the rows to each XCD (2 to 17 % slower); the gradient's next row asked for while one is worked on (0 to 8 % slower); results stored past the
 // caches (2 to 10 % faster alone, but with an addition behind it that reads them 4096 rows of 8192 in bf16 72 -> 79 us).
+// 1024 threads have 128 registers each.  A gradient with an fp32 type among more than 8192 columns, four pieces to a thread, wants more: up to 12 to a thread are spilled where rows are whole, up
+// to 40 where they are odd.
 #include <algorithm>
 
 #include "elements.hpp"
@@ -333,7 +335,7 @@ __global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, in
 }
 
 // Threads to a row, as a power of two: a piece each up to a wavefront's 64, and where rows are few; up to `most` pieces each where they are many.  One and two, us:
-// 16384 bf16 rows of 8192 179 and 186, but 4096 of 2048 12.4 and 10.8, and without a residual 16384 of 4096 53 and 46; 2048 rows of 8192 in 8 bits 27.5 and 24.1; 8192 fp32 rows of
+// 16384 bf16 rows of 8192 179 and 186, but 4096 of 2048 12.4 and 10.8, and without a residual 16384 of 4096 53 and 46; 2048 rows of 8192 in 8 bits, by products alone, 27.5 and 24.1; 8192 fp32 rows of
 // 4096 90 and 93, onto an fp32 stream 71 and 69.  The gradient: 16384 rows of 2048 62 and 54, four pieces in fp32 8191 rows of 4096 134 and 99.
 int threads_of(int pieces, int most, int rows, int least) {
   const int share = rows >= MANY_ROWS ? most : 1;
