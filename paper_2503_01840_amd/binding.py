@@ -419,11 +419,10 @@ def _refuse(what, wanted, t):
 
 
 def _no_tangents(what, *tensors):
-    """The calls that are recorded for autograd have gradients, but no forward-mode derivatives: without this, a dual tensor's tangent would be lost without a word."""
-    if forward_ad._current_level >= 0:                        # a dual_level() is open, which is hardly ever so
-        for t in tensors:
-            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
-                _refuse(what, "a tensor without a forward-mode tangent", t)
+    """Asked while a dual_level() is open.  The calls that are recorded for autograd have gradients, but no forward-mode derivatives: a dual tensor's tangent would be lost without a word."""
+    for t in tensors:
+        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            _refuse(what, "a tensor without a forward-mode tangent", t)
 
 
 def _arg(t, dtype, shape, gpu, what):
@@ -537,7 +536,8 @@ class _Turned(torch.autograd.Function):
 
 
 def _turn(call, back, rope, positions, q, k, out):
-    _no_tangents("q, k, out", q, k, *(out if isinstance(out, (tuple, list)) else (out,)))
+    if forward_ad._current_level >= 0:
+        _no_tangents("q, k, out", q, k, *(out if isinstance(out, (tuple, list)) else (out,)))
     wanted = q.requires_grad or (k is not None and k.requires_grad)
     if out is not None:
         wanted = wanted or any(t is not None and t.requires_grad for t in (out if isinstance(out, (tuple, list)) else (out,)))
@@ -723,7 +723,8 @@ def _workspace(call, sizes, like):
 
 
 def _recorded(*tensors):
-    _no_tangents("inputs", *tensors)
+    if forward_ad._current_level >= 0:
+        _no_tangents("inputs", *tensors)
     for t in tensors:
         if t is not None and t.requires_grad:
             return torch.is_grad_enabled()
@@ -918,7 +919,8 @@ def _teacher(logits, ids, values, lse, t2d, temperature):
     """(gpu, sizes and logits as the calls take them, the teacher's struct)"""
     gpu = _gpu_of(logits, "logits")
     xp, n, V, xs, xc = _table(logits, gpu, "logits")
-    _no_tangents("values, lse", values, lse)
+    if forward_ad._current_level >= 0:
+        _no_tangents("values, lse", values, lse)
     if ids.dim() != 2 or values.requires_grad or (lse is not None and lse.requires_grad):
         _refuse("ids, values, lse", "int32 [rows, k], and fp32 values of which no gradient is wanted", ids)
     k = ids.shape[1]
